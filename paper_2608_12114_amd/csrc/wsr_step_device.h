@@ -1,0 +1,118 @@
+/*
+ * wsr_step_device.h - device building blocks of the step operators (gfx950, wave64): 16-bit
+ * conversions, wave and workgroup reductions, matrix instructions.
+ */
+#ifndef WSR_STEP_DEVICE_H
+#define WSR_STEP_DEVICE_H
+
+#include "wsr_device.h"
+#include "wsr_step_internal.h"
+
+namespace wsr_step {
+
+using wsr::u32x4;
+using wsr::WAVE;
+
+typedef float f4_t __attribute__((ext_vector_type(4)));
+typedef float f16v_t __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
+typedef short s4_t __attribute__((ext_vector_type(4)));
+
+/* 16-byte loads and stores of fp32 rows that are only 4-byte aligned (the hardware takes them) */
+typedef f4_t f4_any_t __attribute__((aligned(4)));
+
+template <int FMT>
+struct Half;
+template <>
+struct Half<WSR_F16> { typedef _Float16 t; typedef wsr::h2_t t2; };
+template <>
+struct Half<WSR_BF16> { typedef __bf16 t; typedef wsr::b2_t t2; };
+
+/* The two 16-bit values of a word, low half first. */
+template <int FMT>
+__device__ __forceinline__ void unpack2(uint32_t v, float& a, float& b) {
+    if constexpr (FMT == WSR_BF16) {
+        a = __uint_as_float(v << 16);
+        b = __uint_as_float(v & 0xffff0000u);
+    } else {
+        const wsr::h2_t h = __builtin_bit_cast(wsr::h2_t, v);
+        a = (float)h.x;
+        b = (float)h.y;
+    }
+}
+
+/* Two values rounded to nearest even and packed. */
+template <int FMT>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    typename Half<FMT>::t2 v;
+    v.x = (typename Half<FMT>::t)a;
+    v.y = (typename Half<FMT>::t)b;
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+template <int FMT>
+__device__ __forceinline__ float unpack1(uint16_t v) {
+    float a, b;
+    unpack2<FMT>(v, a, b);
+    return a;
+}
+
+template <int FMT>
+__device__ __forceinline__ void unpack8(u32x4 w, float (&v)[8]) {
+    unpack2<FMT>(w.x, v[0], v[1]);
+    unpack2<FMT>(w.y, v[2], v[3]);
+    unpack2<FMT>(w.z, v[4], v[5]);
+    unpack2<FMT>(w.w, v[6], v[7]);
+}
+
+/* Sum over a workgroup of WAVES waves, the same bits in every thread: a wave's tree, then the waves in
+   order.  `slot` is a piece of LDS that no other reduction of the kernel uses. */
+template <int WAVES>
+__device__ __forceinline__ float block_sum(float v, float (&slot)[WAVES]) {
+    v = wsr::wave_sum(v);
+    if constexpr (WAVES == 1) return v;
+    if ((threadIdx.x & (WAVE - 1)) == 0) slot[threadIdx.x / WAVE] = v;
+    __syncthreads();
+    float s = slot[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) s += slot[i];
+    return s;
+}
+
+/* Until at most N of the wave's loads (those into LDS among them) are outstanding. */
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int k = 32; k; k >>= 1) v = fmaxf(v, __shfl_xor(v, k));
+    return v;
+}
+
+/* D = A B + C on 16 x 16 x 32: lane l holds row l % 16 of A and column l % 16 of B, elements
+   8 (l / 16) .. + 7 of their 32; D's column l % 16, rows 4 (l / 16) .. + 3. */
+template <int FMT>
+__device__ __forceinline__ f4_t mma_16x16x32(u32x4 a, u32x4 b, f4_t c) {
+    if constexpr (FMT == WSR_BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8_t, a), __builtin_bit_cast(b8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, a), __builtin_bit_cast(h8_t, b), c, 0, 0, 0);
+}
+
+/* D = A B + C on 32 x 32 x 16: lane l holds row l % 32 of A and column l % 32 of B, elements
+   8 (l / 32) .. + 7 of their 16; D's column l % 32, register i row 8 (i / 4) + 4 (l / 32) + i % 4. */
+template <int FMT>
+__device__ __forceinline__ f16v_t mma_32x32x16(u32x4 a, u32x4 b, f16v_t c) {
+    if constexpr (FMT == WSR_BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8_t, a), __builtin_bit_cast(b8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8_t, a), __builtin_bit_cast(h8_t, b), c, 0, 0, 0);
+}
+
+}  // namespace wsr_step
+
+#endif

@@ -236,3 +236,14 @@ def wsr_decode_sweep_ordered(mats, n_tokens: int, ws, ws_bytes: int, framework_s
 
 def wsr_decode_sweep_mma(mats, n_tokens: int, ws, ws_bytes: int, stream=None) -> None:
     _check(_L.wsr_decode_sweep_mma(mats, _n(mats), n_tokens, _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def __getattr__(name):
+    """The entry points of include/wsr_step.h (wsr_block_norm, wsr_lora_sweep, wsr_prefix_attention,
+    wsr_verify_drafts and what belongs to them), from the binding of libwsr_step.so: loaded on first use."""
+    if name.startswith("_"):
+        raise AttributeError(name)
+    from . import wsr_step
+    value = getattr(wsr_step, name)
+    globals()[name] = value
+    return value
