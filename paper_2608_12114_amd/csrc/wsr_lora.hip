@@ -3,15 +3,20 @@
  *
  *   y(t) = y0(t) + s_a B_a (A_a x(t)),  a the adapter of token t.
  *
- * Tokens of one adapter are taken together in tiles, so that an adapter's weights are read once per
- * tile: up to 64 tokens, each workgroup finds its tile from the adapter numbers by ballot; more
- * tokens are sorted by a kernel of one workgroup first.  Then two launches over all projections:
+ * Tokens go in tiles of up to 64; more than 64 are first put in the order of their adapters by a kernel
+ * of one workgroup.  A tile's work is a list of chunks, eight ranks of one adapter each, over all adapters
+ * that its tokens have: whatever the adapters' ranks and however many tokens share one, each chunk's weights
+ * are read once per tile.  Two launches over all projections:
  *
- *   k_lora_shrink   (projection, tile, 64 ranks, part of K): A x on v_mfma_f32_16x16x32, the part's sums
- *                   to the workspace in fp32 (parts keep a single projection spread over the chip)
- *   k_lora_expand   (projection, tile, 256 rows): the parts summed and scaled, then B (A x) on
- *                   v_mfma_f32_16x16x4_f32: B's 16-bit values are exact in fp32 and the inner vector
- *                   keeps its 24 bits, which a 16-bit instruction would cut to 8 or 11
+ *   k_lora_shrink   (tile, span of the projections' K laid end to end): rows of A from two chunks at a time
+ *                   against 16 tokens on v_mfma_f32_16x16x32; a span's sum is stored where the token has the
+ *                   row's adapter.
+ *   k_lora_expand   (projection, tile, rows): four chunks side by side are the 32 terms of one
+ *                   v_mfma_f32_16x16x32; a token's inner vector enters for its own adapter's chunks and as
+ *                   zeros for the others.  The inner vectors are fp32 (24 bits): they enter as the sum of
+ *                   three bf16 terms (24 bits) or of two f16 terms (22 bits, each token's vector scaled by a
+ *                   power of two so that its largest entry is near 2^10), products with B exact, sums fp32.
+ *                   Rounding them to one 16-bit term would leave errors of 2^-9 in the fp32 outputs.
  *
  * Decode is bound by reading the adapters (2 (K + M) rank bytes each), prompts by reading and
  * writing the outputs (8 M bytes per token).
@@ -20,17 +25,20 @@
 
 #include <algorithm>
 
+#include "wsr_mma.h"
 #include "wsr_step_device.h"
 
 namespace wsr_step {
 
 constexpr int LT = 256;                        /* threads per workgroup */
 constexpr int LW = LT / WAVE;
-constexpr int BALLOT_TOKENS = 64;              /* up to here tiles are found by ballot */
-constexpr int EXPAND_ROWS = 256;               /* rows of a workgroup: 64 per wave */
-constexpr int RANKS = 64;                      /* ranks of a shrink workgroup */
+constexpr int TILE = 64;                       /* tokens of a tile */
+constexpr int WINDOW = 64;                     /* ranks worked on at a time */
+constexpr int BLOCK_K = 256;                   /* elements of K that a workgroup's waves take in turn, 64 each */
 constexpr int SORT_THREADS = 1024;
-constexpr int MAX_ADAPTERS = 8192;
+constexpr int SHRINK_HELD = 512, EXPAND_HELD = 512;   /* workgroups on the chip at a time: two per CU */
+typedef u32x4 u32x4_any_t __attribute__((aligned(2)));
+typedef u32x2 u32x2_any_t __attribute__((aligned(2)));
 
 struct LoraMod {
     const void *a, *b, *x;
@@ -38,26 +46,26 @@ struct LoraMod {
     float* y;
     float* v;                                  /* (parts, n_tokens, pitch) partial inner vectors */
     int64_t a_stride, b_stride, x_stride, y0_stride, y_stride, M, K;
-    int32_t rank, pitch, parts, part_k;        /* pitch: rank up to a multiple of 16 */
+    int32_t rank, pitch, parts, block0;        /* pitch: rank up to a multiple of 8; block0: its first block of K */
 };
 static_assert(sizeof(LoraMod) == 120, "LoraMod layout");
 
-/* Projections and the first workgroup of each, in the launch arguments. */
+/* Projections and the first unit of work of each, in the launch arguments. */
 template <int N>
 struct LoraTable {
-    int32_t n;
+    int32_t n, units;
     int32_t first[N];
     LoraMod mod[N];
 };
 
 struct LoraCall {
-    const int32_t *adapter_of, *ranks, *tiles; /* tiles: null by ballot; else count, then (adapter, first, tokens), then the order */
+    const int32_t *adapter_of, *ranks, *order; /* order: null where tokens are taken as they come */
     const float* scales;
-    const int32_t* order;
-    int32_t n_tokens, n_adapters, tile_slots;  /* tiles of the grid per projection */
+    int32_t n_tokens, n_adapters, tiles;
+    int32_t span, slots;                       /* blocks of a shrink workgroup; workgroups that share its rows */
 };
 
-/* The projection that workgroup b belongs to: the last whose first workgroup is <= b. */
+/* The projection that unit b belongs to: the last whose first unit is <= b. */
 template <int N>
 __device__ __forceinline__ int mod_of(const LoraTable<N>& tab, int b) {
     const int lane = threadIdx.x % WAVE;
@@ -70,187 +78,471 @@ __device__ __forceinline__ int mod_of(const LoraTable<N>& tab, int b) {
     return __builtin_amdgcn_readfirstlane(m) - 1;
 }
 
-/* Tile `tile` of the call: its adapter, rank and tokens (toks, -1 beyond them); false if there is none. */
+/* A tile in LDS.  A chunk of its list: adapter << 8 | (eighth of the window) << 4 | ranks it holds (1 to 8). */
 template <int COLS>
-__device__ __forceinline__ bool find_tile(const LoraCall& c, int tile, int rank, int (&toks)[COLS], int& adapter, int& r) {
-    const int lane = threadIdx.x % WAVE;
-    int count;
-    if (!c.tiles) {
-        const int id = lane < c.n_tokens ? c.adapter_of[lane] : -2;
-        const bool has = id >= 0 && id < c.n_adapters;
-        const int key = lane < c.n_tokens ? (has ? id : -1) : -2;
-        adapter = __builtin_amdgcn_readlane(key, tile);
-        const uint64_t mine = __ballot(key == adapter);
-        const int before = __builtin_popcountll(mine & ((1ull << tile) - 1));
-        if (before % COLS) return false;              /* not the first token of a tile */
-        const int at = __builtin_popcountll(mine & ((1ull << lane) - 1)) - before;
-        count = min(COLS, (int)__builtin_popcountll(mine) - before);
-        if (threadIdx.x < WAVE) {
-            if (lane < COLS) toks[lane] = -1;
-            if (key == adapter && at >= 0 && at < COLS) toks[at] = lane;
+struct Tile {
+    int32_t list[COLS * (WINDOW / 8)];
+    int32_t tok[COLS], id[COLS], rank[COLS];   /* -1: no token, no adapter (or none of its ranks) */
+    float scale[COLS];
+    int32_t chunks, mixed, partial;            /* mixed: tokens of more than one adapter; partial: a chunk under 8 ranks */
+};
+
+/* The tile's tokens and the chunks of ranks w0 .. w0 + WINDOW - 1, by the first wave. */
+template <int COLS>
+__device__ __forceinline__ void make_tile(const LoraCall& c, int tile, int rank, int w0, Tile<COLS>& t) {
+    if (threadIdx.x < WAVE) {
+        const int lane = threadIdx.x, at = tile * TILE + lane;
+        const bool in = lane < COLS && at < c.n_tokens;
+        const int tok = in ? (c.order ? c.order[at] : at) : -1;
+        int id = in ? c.adapter_of[tok] : -1, r = 0;
+        if (id < 0 || id >= c.n_adapters) id = -1;
+        if (id >= 0) {
+            r = c.ranks ? min(max(c.ranks[id], 0), rank) : rank;
+            if (r == 0) id = -1;
         }
-    } else {
-        if (tile >= c.tiles[0]) return false;
-        adapter = __builtin_amdgcn_readfirstlane(c.tiles[1 + 3 * tile]);
-        const int first = c.tiles[2 + 3 * tile];
-        count = c.tiles[3 + 3 * tile];
-        for (int i = threadIdx.x; i < COLS; i += LT) toks[i] = i < count ? c.order[first + i] : -1;
+        bool first = id >= 0;                  /* of its adapter in the tile */
+        if (c.order) {
+            const int before = __shfl_up(id, 1);
+            if (lane > 0 && before == id) first = false;
+        } else {
+            const int n = min(COLS, c.n_tokens);
+            for (int j = 0; j < n; ++j)
+                if (j < lane && __builtin_amdgcn_readlane(id, j) == id) first = false;
+        }
+        const int mine = first ? (min(max(r - w0, 0), WINDOW) + 7) / 8 : 0;
+        int sum = mine;
+#pragma unroll
+        for (int k = 1; k < WAVE; k <<= 1) {
+            const int o = __shfl_up(sum, k);
+            if (lane >= k) sum += o;
+        }
+        for (int k = 0; k < mine; ++k) t.list[sum - mine + k] = id << 8 | k << 4 | min(8, r - w0 - 8 * k);
+        const int all = __shfl(sum, WAVE - 1);
+        if (lane < COLS) {
+            t.tok[lane] = tok, t.id[lane] = id, t.rank[lane] = r;
+            t.scale[lane] = id >= 0 && c.scales ? c.scales[id] : 1.f;
+        }
+        const int adapters = __builtin_popcountll(__ballot(first));
+        const bool odd = __ballot(first && r % 8) != 0;
+        if (lane == 0) t.chunks = all, t.mixed = adapters > 1, t.partial = odd;
     }
-    r = adapter < 0 ? 0 : c.ranks ? min(max(c.ranks[adapter], 0), rank) : rank;
-    r = __builtin_amdgcn_readfirstlane(r);
     __syncthreads();
-    return true;
 }
 
-template <int FMT, int NT, int N>
+/* 16 bytes of weights, past the caches where a single tile reads them. */
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load_weights(const char* p) {
+    typedef const __attribute__((address_space(1))) u32x4_any_t g_any;
+    if constexpr (ONCE) return __builtin_nontemporal_load((g_any*)p);
+    else return *(g_any*)p;
+}
+
+/* The units of work of a workgroup: a contiguous share of all, so that it meets few projections and makes
+   its tile once. */
+__device__ __forceinline__ void share_of(int units, int tiles, int& tile, int& u0, int& u1) {
+    const int groups = gridDim.x / tiles, i = blockIdx.x / tiles;
+    tile = blockIdx.x % tiles;
+    u0 = (int)((int64_t)units * i / groups);
+    u1 = (int)((int64_t)units * (i + 1) / groups);
+}
+
+/* Rows of A are rows of the product and tokens its columns, so what stands in the rows past a chunk's ranks
+   or in columns without a token reaches no stored sum: their pointers are set to a valid row.  Past K both
+   sides are zeros. */
+template <int FMT, int TT, int RT, int N>
 __global__ __launch_bounds__(LT) void k_lora_shrink(LoraTable<N> tab, LoraCall c) {
-    constexpr int RT = RANKS / 16;
-    __shared__ int toks[16 * NT];
-    __shared__ f4_t red[LW][RT * NT][WAVE];
-    const int m = mod_of(tab, blockIdx.x);
-    const LoraMod& d = tab.mod[m];
-    int at = blockIdx.x - tab.first[m];
-    const int part = at % d.parts;
-    at /= d.parts;
-    const int blocks = (d.rank + RANKS - 1) / RANKS, r0 = at % blocks * RANKS, tile = at / blocks;
-    int adapter, r;
-    if (!find_tile<16 * NT>(c, tile, d.rank, toks, adapter, r) || r0 >= r) return;
+    constexpr int COLS = 16 * TT;
+    __shared__ Tile<COLS> t;
+    __shared__ f4_t red[LW][RT * TT][WAVE];
     const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), col = lane % 16, g = lane / 16;
-    const char* a = (const char*)d.a + adapter * d.a_stride;
-    const int64_t k0 = (int64_t)part * d.part_k, k1 = min(d.K, k0 + d.part_k);
-    const char* xr[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) xr[t] = toks[16 * t + col] < 0 ? nullptr : (const char*)d.x + toks[16 * t + col] * d.x_stride;
-    const int tiles_r = (min(RANKS, r - r0) + 15) / 16;
-    f4_t acc[RT][NT] = {};
-    for (int64_t k = k0 + wave * 32; k < k1; k += 32 * LW) {
-        const int64_t kk = k + 8 * g;
-        u32x4 xv[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) xv[t] = kk < k1 && xr[t] ? *(const u32x4*)(xr[t] + kk * 2) : wsr::zero4();
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            if (i >= tiles_r) break;
-            const int j = r0 + 16 * i + col;
-            const u32x4 av = kk < k1 && j < r ? *(const u32x4*)(a + (j * d.K + kk) * 2) : wsr::zero4();
-#pragma unroll
-            for (int t = 0; t < NT; ++t) acc[i][t] = mma_16x16x32<FMT>(av, xv[t], acc[i][t]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) red[wave][i * NT + t][lane] = acc[i][t];
-    __syncthreads();
-    for (int e = wave; e < tiles_r * NT; e += LW) {
-        const int i = e / NT, t = e % NT, tok = toks[16 * t + col];
-        f4_t s = red[0][e][lane];
-#pragma unroll
-        for (int w = 1; w < LW; ++w) s += red[w][e][lane];
-        if (tok >= 0) *(f4_t*)(d.v + ((int64_t)part * c.n_tokens + tok) * d.pitch + r0 + 16 * i + 4 * g) = s;
-    }
-}
-
-/* Four consecutive 16-bit values of a row of B as fp32, those from `left` on as zeros. */
-template <int FMT>
-__device__ __forceinline__ f4_t load_b4(const char* p, int left, bool wide) {
-    if (left <= 0) return f4_t{0, 0, 0, 0};
-    uint32_t w0 = 0, w1 = 0;
-    if (wide && left >= 4) {
-        const u32x2 w = *(const u32x2*)p;
-        w0 = w.x, w1 = w.y;
-    } else {
-        const uint16_t* q = (const uint16_t*)p;
-        w0 = q[0];
-        if (left > 1) w0 |= (uint32_t)q[1] << 16;
-        if (left > 2) w1 = q[2];
-        if (left > 3) w1 |= (uint32_t)q[3] << 16;
-    }
-    float o0, o1, o2, o3;
-    unpack2<FMT>(w0, o0, o1);
-    unpack2<FMT>(w1, o2, o3);
-    return f4_t{o0, o1, o2, o3};
-}
-
-constexpr int VRANKS = 128;                    /* ranks of the inner vectors held in LDS at a time */
-constexpr int VPAD = 4;                        /* floats between their rows */
-
-template <int FMT, int NT, int N>
-__global__ __launch_bounds__(LT) void k_lora_expand(LoraTable<N> tab, LoraCall c) {
-    __shared__ float vs[16 * NT * (VRANKS + VPAD)];
-    __shared__ int toks[16 * NT];
-    const int m = mod_of(tab, blockIdx.x);
-    const LoraMod& d = tab.mod[m];
-    int at = blockIdx.x - tab.first[m];
-    const int blocks = (int)((d.M + EXPAND_ROWS - 1) / EXPAND_ROWS), tile = at / blocks;
-    const int64_t row0 = (int64_t)(at % blocks) * EXPAND_ROWS;
-    int adapter, r;
-    if (!find_tile<16 * NT>(c, tile, d.rank, toks, adapter, r)) return;
-    if (r == 0 && d.y0 == d.y) return;         /* y already holds the result */
-    const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), col = lane % 16, g = lane / 16;
-    const float scale = adapter >= 0 && c.scales ? c.scales[adapter] : 1.f;
-    const char* b = (const char*)d.b + (adapter < 0 ? 0 : adapter) * d.b_stride;
-    const bool wide = d.rank % 4 == 0 && ((uintptr_t)b & 7) == 0;
-    const int64_t i0 = row0 + wave * 64;
-    f4_t acc[4][NT] = {};
-    for (int j0 = 0; j0 < r; j0 += VRANKS) {
-        const int q = (min(r - j0, VRANKS) + 15) / 16 * 4;     /* groups of four ranks of this round */
-        if (j0) __syncthreads();
-        for (int e = threadIdx.x; e < 16 * NT * q; e += LT) {
-            const int tok = toks[e / q], j = e % q * 4;
-            f4_t s = {0, 0, 0, 0};
-            if (tok >= 0)
-                for (int p = 0; p < d.parts; ++p)
-                    s += *(const f4_t*)(d.v + ((int64_t)p * c.n_tokens + tok) * d.pitch + j0 + j);
-            *(f4_t*)(vs + (e / q) * (VRANKS + VPAD) + j) = s * scale;
-        }
-        __syncthreads();
-        for (int j = 0; j < 4 * q; j += 16) {
-            const int jj = j + 4 * g;
-            f4_t bv[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t row = i0 + 16 * i + col;
-                bv[i] = load_b4<FMT>(b + (row * d.rank + j0 + jj) * 2, row < d.M ? r - j0 - jj : 0, wide);
+    int made = -1;
+    const int tile = blockIdx.x % c.tiles, slot = blockIdx.x / c.tiles % c.slots, span = blockIdx.x / c.tiles / c.slots;
+    const int from = span * c.span, to = min(tab.units, from + c.span);
+    int m = mod_of(tab, from);
+    for (int block = from; block < to; ++m) {
+        const LoraMod& d = tab.mod[m];
+        const int end = m + 1 < tab.n ? min(to, tab.first[m + 1]) : to;    /* of the blocks in this projection */
+        const int part = span - d.block0 / c.span;
+        const int k0 = (block - d.block0) * BLOCK_K, k1 = (int)min(d.K, (int64_t)(end - d.block0) * BLOCK_K);
+        block = end;
+        if (k0 >= k1 && d.K > 0) continue;
+        for (int w0 = 0; w0 < d.rank; w0 += WINDOW) {
+            if (made != d.rank || d.rank > WINDOW) {
+                __syncthreads();
+                make_tile<COLS>(c, tile, d.rank, w0, t);
+                made = d.rank;
             }
+            /* a load takes 128 bytes of each of eight rows (eight tokens): lane (g, col) those at 16 (g + 4 (col / 8)) */
+            const int lane_at = 16 * (g + col / 8 * 4);
+            const char* xr[TT][2];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const f4_t vv = *(const f4_t*)(vs + (16 * t + col) * (VRANKS + VPAD) + jj);
+            for (int i = 0; i < TT; ++i)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int b = 0; b < 2; ++b) {
+                    const int tok = t.tok[16 * i + 8 * b + col % 8];
+                    xr[i][b] = (const char*)d.x + (tok < 0 ? t.tok[0] : tok) * d.x_stride + lane_at;
+                }
+            for (int c0 = slot * 2 * RT; c0 < t.chunks; c0 += c.slots * 2 * RT) {
+                const char *ar[RT][2], *xp[TT][2];
+#pragma unroll
+                for (int i = 0; i < TT; ++i) xp[i][0] = xr[i][0], xp[i][1] = xr[i][1];
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int ch = t.list[min(c0 + 2 * i + b, t.chunks - 1)];
+                        const int j = w0 + (ch >> 4 & 15) * 8 + min(col % 8, (ch & 15) - 1);
+                        ar[i][b] = (const char*)d.a + (ch >> 8) * d.a_stride + j * d.K * 2 + lane_at;
+                    }
+                f4_t acc[RT][TT] = {};
+                /* a batch, 64 elements of every row, is loaded while the one before it is multiplied */
+                struct Batch {
+                    u32x4 a[RT][2], x[TT][2];
+                };
+                Batch b0, b1;
+                auto load = [&](Batch& b, int ahead) {     /* `ahead` bytes, a constant */
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) b.a[i][h] = load_weights<TT == 1>(ar[i][h] + ahead);
+#pragma unroll
+                        for (int i = 0; i < TT; ++i) b.x[i][h] = *(const u32x4*)(xp[i][h] + ahead);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                auto advance = [&](int by) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) ar[i][h] += by;
+#pragma unroll
+                        for (int i = 0; i < TT; ++i) xp[i][h] += by;
+                    }
+                };
+                auto multiply = [&](Batch& b) {
+#pragma unroll
+                    for (int i = 0; i < TT; ++i) wsr::lines_to_slabs(b.x[i][0], b.x[i][1]);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        wsr::lines_to_slabs(b.a[i][0], b.a[i][1]);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int j = 0; j < TT; ++j) acc[i][j] = mma_16x16x32<FMT>(b.a[i][h], b.x[j][h], acc[i][j]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                constexpr int B = BLOCK_K / LW, S = BLOCK_K;
+                int k = k0 + wave * B;
+                advance(k * 2);
+                if constexpr (TT > 1) {        /* no registers for two batches */
+                    for (; k + B <= k1; k += S) {
+                        load(b0, 0);
+                        multiply(b0);
+                        advance(S * 2);
+                    }
+                } else if (k + B <= k1) {
+                    load(b0, 0);
+                    for (; k + 2 * S + B <= k1; k += 2 * S) {
+                        load(b1, S * 2);
+                        multiply(b0);
+                        advance(S * 4);
+                        load(b0, 0);
+                        multiply(b1);
+                    }
+                    if (k + S + B <= k1) {
+                        load(b1, S * 2);
+                        multiply(b0);
+                        multiply(b1);
+                        k += 2 * S;
+                        advance(S * 4);
+                    } else {
+                        multiply(b0);
+                        k += S;
+                        advance(S * 2);
+                    }
+                }
+                if (k < k1) {                  /* the last elements, fewer than a batch */
+                    const bool in = k + 8 * (g + col / 8 * 4) < k1;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) b0.a[i][h] = in ? *(const u32x4*)ar[i][h] : wsr::zero4();
+#pragma unroll
+                        for (int i = 0; i < TT; ++i) b0.x[i][h] = in ? *(const u32x4*)xp[i][h] : wsr::zero4();
+                    }
+                    multiply(b0);
+                }
+                __syncthreads();               /* the round before has been read */
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int j = 0; j < TT; ++j) red[wave][i * TT + j][lane] = acc[i][j];
+                __syncthreads();
+                for (int e = wave; e < RT * TT; e += LW) {
+                    const int cell = c0 + 2 * (e / TT) + g / 2, token = 16 * (e % TT) + col;
+                    if (cell >= t.chunks) continue;
+                    const int ch = t.list[cell];
+                    if (t.id[token] != ch >> 8) continue;
+                    f4_t s = red[0][e][lane];
+#pragma unroll
+                    for (int w = 1; w < LW; ++w) s += red[w][e][lane];
+                    *(f4_t*)(d.v + ((int64_t)part * c.n_tokens + t.tok[token]) * d.pitch + w0 + (ch >> 4 & 15) * 8 + 4 * (g % 2)) = s;
+                }
+            }
+        }
+    }
+}
+
+/* Eight 16-bit values of a row of B of which `n` count; the others are zeros. */
+__device__ __forceinline__ u32x4 load_chunk_row(const char* p, int n) {
+    if (n == 8) return *(const u32x4_any_t*)p;
+    u32x4 o = wsr::zero4();
+    const uint16_t* q = (const uint16_t*)p;
+    if (n >= 4) {
+        const u32x2 w = *(const u32x2_any_t*)p;
+        o.x = w.x, o.y = w.y;
+        if (n > 4) o.z = q[4];
+        if (n > 5) o.z |= (uint32_t)q[5] << 16;
+        if (n > 6) o.w = q[6];
+    } else {
+        if (n > 0) o.x = q[0];
+        if (n > 1) o.x |= (uint32_t)q[1] << 16;
+        if (n > 2) o.y = q[2];
+    }
+    return o;
+}
+
+/* Nonzero where one of the eight values is an infinity or NaN (all ones in the exponent). */
+template <int FMT>
+__device__ __forceinline__ uint32_t not_finite(u32x4 w) {
+    constexpr uint32_t E = FMT == WSR_BF16 ? 0x7f807f80u : 0x7c007c00u, ONE = FMT == WSR_BF16 ? 0x00800080u : 0x04000400u;
+    return (((w.x & E) + ONE) | ((w.y & E) + ONE) | ((w.z & E) + ONE) | ((w.w & E) + ONE)) & 0x80008000u;
+}
+
+template <int FMT>
+constexpr int terms() { return FMT == WSR_BF16 ? 3 : 2; }
+
+/* The inner vectors of a window in LDS as 16-bit terms, and the power of two that undoes each token's
+   scaling.  A pitch of 16 bytes past a multiple of 128 keeps the 16 tokens' reads on different banks. */
+template <int FMT, int COLS>
+struct Inner {
+    static constexpr int PITCH = terms<FMT>() * WINDOW + 8;
+    uint16_t v[COLS * PITCH];
+    float undo[COLS];
+};
+
+template <int FMT, int COLS>
+__device__ __forceinline__ void make_inner(const LoraMod& d, const LoraCall& c, const Tile<COLS>& t, int w0, Inner<FMT, COLS>& in) {
+    typedef Inner<FMT, COLS> I;
+    const int q = threadIdx.x % 16;            /* sixteen lanes take a token, four ranks each */
+    const int pitch = d.pitch;
+    auto load = [&](int token, int j) {
+        f4_t s = {0, 0, 0, 0};
+        const int r = t.id[token] < 0 ? 0 : t.rank[token];
+        if (j < r) {
+            const float* p = d.v + (int64_t)t.tok[token] * pitch + j;
+            const int64_t next = (int64_t)c.n_tokens * pitch;
+            int k = 0;
+            for (; k + 4 <= d.parts; k += 4, p += 4 * next)
+                s += (*(const f4_t*)p + *(const f4_t*)(p + next)) + (*(const f4_t*)(p + 2 * next) + *(const f4_t*)(p + 3 * next));
+            if (k + 2 <= d.parts) s += *(const f4_t*)p + *(const f4_t*)(p + next), k += 2, p += 2 * next;
+            if (k < d.parts) s += *(const f4_t*)p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] = j + e < r ? s[e] * t.scale[token] : 0.f;
+        }
+        return s;
+    };
+    for (int token = threadIdx.x / 16; token < COLS; token += LT / 16) {
+        f4_t s = load(token, w0 + 4 * q);
+        if constexpr (FMT == WSR_F16) {
+            float top = 0.f;
+            if (d.rank <= WINDOW) top = fmaxf(fmaxf(fabsf(s[0]), fabsf(s[1])), fmaxf(fabsf(s[2]), fabsf(s[3])));
+            else
+                for (int w = 0; w < d.rank; w += WINDOW) {
+                    const f4_t o = load(token, w + 4 * q);
+                    top = fmaxf(top, fmaxf(fmaxf(fabsf(o[0]), fabsf(o[1])), fmaxf(fabsf(o[2]), fabsf(o[3]))));
+                }
+#pragma unroll
+            for (int k = 1; k < 16; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+            /* 2^9 <= scaled top < 2^10, the exponent kept where both powers of two are normal */
+            const int e = top > 0.f && top < __builtin_inff() ? min(max(10 - __builtin_amdgcn_frexp_expf(top), -110), 110) : 0;
+            s *= __builtin_amdgcn_ldexpf(1.f, e);
+            if (q == 0) in.undo[token] = __builtin_amdgcn_ldexpf(1.f, -e);
+        }
+#pragma unroll
+        for (int k = 0; k < terms<FMT>(); ++k) {
+            typedef typename Half<FMT>::t H;
+            u32x2 w;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                w[e] = pack2<FMT>(s[2 * e], s[2 * e + 1]);
+                const float a = s[2 * e] - (float)(H)s[2 * e], b = s[2 * e + 1] - (float)(H)s[2 * e + 1];
+                s[2 * e] = a == a ? a : 0.f, s[2 * e + 1] = b == b ? b : 0.f;   /* inf - inf */
+            }
+            *(u32x2*)(in.v + token * I::PITCH + k * WINDOW + 4 * q) = w;
+        }
+    }
+    __syncthreads();
+}
+
+/* A wave's 16 RW rows of a unit against the tile's tokens, U steps of four chunks at a time. */
+template <int FMT, int TT, int RW, int N>
+__global__ __launch_bounds__(LT) void k_lora_expand(LoraTable<N> tab, LoraCall c) {
+    constexpr int COLS = 16 * TT, ROWS = LW * 16 * RW, U = TT == 1 ? 16 / RW : 2, NTERM = terms<FMT>();
+    typedef Inner<FMT, COLS> I;
+    __shared__ Tile<COLS> t;
+    __shared__ I in;
+    const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), col = lane % 16, g = lane / 16;
+    int tile, u0, u1, made = -1, inner = -1;
+    share_of(tab.units, c.tiles, tile, u0, u1);
+    if (u0 >= u1) return;
+    const int used = min(TT, (c.n_tokens - tile * TILE + 15) / 16);    /* token tiles that hold tokens */
+    int m = mod_of(tab, u0);
+    for (int unit = u0; unit < u1; ++unit) {
+        while (m + 1 < tab.n && tab.first[m + 1] <= unit) ++m;
+        const LoraMod& d = tab.mod[m];
+        const int64_t i0 = (int64_t)(unit - tab.first[m]) * ROWS + wave * 16 * RW;
+        const bool whole = i0 + 16 * RW <= d.M;
+        f4_t acc[RW][TT] = {}, y0[RW][TT];
+        for (int w0 = 0; w0 < d.rank; w0 += WINDOW) {
+            if (made != d.rank || d.rank > WINDOW) {
+                __syncthreads();
+                make_tile<COLS>(c, tile, d.rank, w0, t);
+                made = d.rank;
+            }
+            if (w0 == 0 && whole && d.y0) {
+#pragma unroll
+                for (int j = 0; j < TT; ++j) {
+                    const int tok = t.tok[16 * j + col];
+                    const float* src = (const float*)((const char*)d.y0 + (tok < 0 ? t.tok[0] : tok) * d.y0_stride) + i0 + 4 * g;
+#pragma unroll
+                    for (int i = 0; i < RW; ++i) y0[i][j] = *(const f4_any_t*)(src + 16 * i);
+                }
+            }
+            if (t.chunks == 0) break;          /* no adapter reaches this window or a later one */
+            if (inner != m || d.rank > WINDOW) {
+                __syncthreads();
+                make_inner<FMT, COLS>(d, c, t, w0, in);
+                inner = m;
+            }
+            int id[TT];
+#pragma unroll
+            for (int j = 0; j < TT; ++j) id[j] = t.id[16 * j + col];
+            const bool partial = __builtin_amdgcn_readfirstlane(t.partial), mixed = __builtin_amdgcn_readfirstlane(t.mixed);
+            const int chunks = __builtin_amdgcn_readfirstlane(t.chunks);
+            int64_t row[RW];
+#pragma unroll
+            for (int i = 0; i < RW; ++i) row[i] = min(i0 + 16 * i + col, d.M - 1) * d.rank * 2;
+            for (int c0 = 0; c0 < chunks; c0 += 4 * U) {
+                int adapter[U];
+                /* past the list's end the last chunk stands in, against no token */
+                u32x4 b[U][RW];
+                int ch[U];
+                const char* p[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int cell = c0 + 4 * u + g;
+                    ch[u] = t.list[min(cell, chunks - 1)];
+                    p[u] = (const char*)d.b + (ch[u] >> 8) * d.b_stride + (w0 + (ch[u] >> 4 & 15) * 8) * 2;
+                    adapter[u] = cell < chunks ? ch[u] >> 8 : -2;
+                }
+                if (partial) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int i = 0; i < RW; ++i) b[u][i] = load_chunk_row(p[u] + row[i], ch[u] & 15);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int i = 0; i < RW; ++i) b[u][i] = load_weights<TT == 1>(p[u] + row[i]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                /* zero times an infinity or NaN of one adapter's weights would reach the tokens of the others:
+                   such chunks go one by one, their sums taken over by their own tokens only */
+                bool apart = false;
+                if (mixed) {
+                    uint32_t bad = 0;
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int i = 0; i < RW; ++i) bad |= not_finite<FMT>(b[u][i]);
+                    apart = __ballot(bad != 0) != 0;
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (c0 + 4 * u >= chunks) break;
+                    const int chunk = (ch[u] >> 4 & 15) * 8;
+#pragma unroll
+                    for (int j = 0; j < TT; ++j) {
+                        if (j >= used) break;
+                        const bool own = id[j] == adapter[u];
+                        if (__ballot(own) == 0) continue;
+                        u32x4 v[NTERM];
+#pragma unroll
+                        for (int k = 0; k < NTERM; ++k) {
+                            v[k] = *(const u32x4*)(in.v + (16 * j + col) * I::PITCH + k * WINDOW + chunk);
+                            if (!own) v[k] = wsr::zero4();
+                        }
+                        if (!apart) {
+#pragma unroll
+                            for (int k = 0; k < NTERM; ++k)
+#pragma unroll
+                                for (int i = 0; i < RW; ++i) acc[i][j] = mma_16x16x32<FMT>(b[u][i], v[k], acc[i][j]);
+                        } else {
+                            for (int o = 0; o < 4; ++o) {
+                                const bool mine = id[j] >= 0 && id[j] == __shfl(adapter[u], 16 * o);
+#pragma unroll
+                                for (int i = 0; i < RW; ++i) {
+                                    f4_t s = acc[i][j];
+#pragma unroll
+                                    for (int k = 0; k < NTERM; ++k)
+                                        s = mma_16x16x32<FMT>(g == o ? b[u][i] : wsr::zero4(), g == o ? v[k] : wsr::zero4(), s);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) acc[i][j][e] = mine ? s[e] : acc[i][j][e];
+                                }
+                            }
+                        }
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < TT; ++j) {
+            const int tok = t.tok[16 * j + col];
+            const bool has = t.id[16 * j + col] >= 0;
+            if (tok < 0 || (!has && d.y0 == d.y)) continue;
+            const float undo = FMT == WSR_F16 && has ? in.undo[16 * j + col] : 1.f;
+            float* dst = (float*)((char*)d.y + tok * d.y_stride) + i0 + 4 * g;
+            if (whole) {
+#pragma unroll
+                for (int i = 0; i < RW; ++i) {
+                    f4_t s = acc[i][j] * undo;
+                    if (d.y0) s = has ? y0[i][j] + s : y0[i][j];
+                    *(f4_any_t*)(dst + 16 * i) = s;
+                }
+            } else {
+                const float* src = d.y0 ? (const float*)((const char*)d.y0 + tok * d.y0_stride) + i0 + 4 * g : nullptr;
+#pragma unroll
+                for (int i = 0; i < RW; ++i)
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        acc[i][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(bv[i][k], vv[k], acc[i][t], 0, 0, 0);
-            }
-        }
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int tok = toks[16 * t + col];
-        if (tok < 0) continue;
-        const float* src = d.y0 ? (const float*)((const char*)d.y0 + tok * d.y0_stride) : nullptr;
-        float* dst = (float*)((char*)d.y + tok * d.y_stride);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t o = i0 + 16 * i + 4 * g;
-            if (o + 4 <= d.M) {
-                f4_t s = acc[i][t];
-                if (src) s += *(const f4_any_t*)(src + o);
-                *(f4_any_t*)(dst + o) = s;
-            } else {
-                for (int k = 0; o + k < d.M; ++k) dst[o + k] = acc[i][t][k] + (src ? src[o + k] : 0.f);
+                        if (i0 + 16 * i + 4 * g + k < d.M) {
+                            const float s = acc[i][j][k] * undo;
+                            dst[16 * i + k] = !src ? s : has ? src[16 * i + k] + s : src[16 * i + k];
+                        }
             }
         }
     }
 }
 
-/* Tokens in order of their adapters (those without one last) and the tiles of `cols` tokens.  The order
-   inside an adapter follows from the atomics and may differ from run to run; a token's results do not
-   depend on its place in a tile. */
+/* Tokens in the order of their adapters, those without one last.  The order inside an adapter follows from
+   the atomics and may differ from run to run; a token's results do not depend on its place in a tile. */
 __global__ __launch_bounds__(SORT_THREADS) void k_lora_sort(const int32_t* adapter_of, int n_tokens, int n_adapters,
-                                                            int cols, int32_t* tiles, int32_t* order) {
+                                                            int32_t* order) {
     extern __shared__ int32_t bin[];           /* [n_adapters + 1] */
-    __shared__ int32_t sc[SORT_THREADS], st[SORT_THREADS];
+    __shared__ int32_t sc[SORT_THREADS];
     const int n = n_adapters + 1, tid = threadIdx.x;
     for (int i = tid; i < n; i += SORT_THREADS) bin[i] = 0;
     __syncthreads();
@@ -260,25 +552,19 @@ __global__ __launch_bounds__(SORT_THREADS) void k_lora_sort(const int32_t* adapt
     }
     __syncthreads();
     const int per = (n + SORT_THREADS - 1) / SORT_THREADS, b0 = min(n, tid * per), b1 = min(n, b0 + per);
-    int tokens = 0, made = 0;
-    for (int i = b0; i < b1; ++i) tokens += bin[i], made += (bin[i] + cols - 1) / cols;
-    sc[tid] = tokens, st[tid] = made;
+    int tokens = 0;
+    for (int i = b0; i < b1; ++i) tokens += bin[i];
+    sc[tid] = tokens;
     __syncthreads();
     for (int k = 1; k < SORT_THREADS; k <<= 1) {
-        const int a = tid >= k ? sc[tid - k] : 0, b = tid >= k ? st[tid - k] : 0;
+        const int a = tid >= k ? sc[tid - k] : 0;
         __syncthreads();
-        sc[tid] += a, st[tid] += b;
+        sc[tid] += a;
         __syncthreads();
     }
-    if (tid == SORT_THREADS - 1) tiles[0] = st[tid];
-    int at = sc[tid] - tokens, tile = st[tid] - made;
+    int at = sc[tid] - tokens;
     for (int i = b0; i < b1; ++i) {
         const int count = bin[i];
-        for (int k = 0; k < count; k += cols, ++tile) {
-            tiles[1 + 3 * tile] = i == n_adapters ? -1 : i;
-            tiles[2 + 3 * tile] = at + k;
-            tiles[3 + 3 * tile] = min(cols, count - k);
-        }
         bin[i] = at;
         at += count;
     }
@@ -291,57 +577,110 @@ __global__ __launch_bounds__(SORT_THREADS) void k_lora_sort(const int32_t* adapt
 
 /* ---- host ------------------------------------------------------------------------------------------ */
 
-static int tile_cols(int32_t n_tokens) { return n_tokens <= BALLOT_TOKENS ? 16 : 64; }
-static int64_t most_tiles(int32_t n_tokens, int32_t n_adapters) {
-    if (n_tokens <= BALLOT_TOKENS) return n_tokens;
-    return n_tokens / tile_cols(n_tokens) + std::min<int64_t>(n_tokens, (int64_t)n_adapters + 1);
-}
+static int tiles_of(int32_t n_tokens) { return (n_tokens + TILE - 1) / TILE; }
 
-/* Parts of K of each projection: enough workgroups to fill the chip where the call is small, none under
-   512 elements. */
-static void part_of(const wsr_lora& m, int32_t n, int32_t n_tokens, int& parts, int& part_k) {
-    const int64_t tiles = std::max<int64_t>(1, n_tokens / tile_cols(n_tokens));
-    const int64_t want = std::max<int64_t>(1, 512 / (tiles * n)), most = std::max<int64_t>(1, (m.K + 511) / 512);
-    const int64_t k = (m.K + std::min(want, most) - 1) / std::min(want, most);
-    part_k = (int)std::max<int64_t>(32, (k + 31) / 32 * 32);
-    parts = (int)std::max<int64_t>(1, (m.K + part_k - 1) / part_k);
+/* The blocks of K of a shrink workgroup's span, and with them each projection's parts: spans that give every
+   workgroup the chip holds (two per CU) an equal share, of two blocks at least; for many tokens so long that a
+   token's parts, which the second launch adds up once per workgroup and projection, stay within 2 KiB. */
+static int64_t blocks_of(const wsr_lora& m) { return std::max<int64_t>(1, (m.K + BLOCK_K - 1) / BLOCK_K); }
+static int span_of(const wsr_lora* mods, int32_t n, int32_t n_tokens) {
+    int64_t all = 0, least = 2;
+    for (int32_t i = 0; i < n; ++i) {
+        all += blocks_of(mods[i]);
+        if (n_tokens > TILE) least = std::max(least, blocks_of(mods[i]) / std::max(1, 512 / mods[i].rank));
+    }
+    const int64_t held = std::max<int64_t>(1, SHRINK_HELD / tiles_of(n_tokens));
+    return (int)std::min<int64_t>(1 << 24, std::max(least, (all + held - 1) / held));
 }
 
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-static size_t lists_bytes(int32_t n_tokens) {
-    return n_tokens <= BALLOT_TOKENS ? 0 : up256(4 * (1 + 3 * (size_t)most_tiles(n_tokens, MAX_ADAPTERS))) + up256(4 * (size_t)n_tokens);
+static size_t order_bytes(int32_t n_tokens) { return n_tokens <= TILE ? 0 : up256(4 * (size_t)n_tokens); }
+constexpr int TABLE_MAX = 224;
+
+/* Runs of projections that one pair of launches takes: of one type, at most a table's length. */
+static int32_t run_of(const wsr_lora* mods, int32_t n) {
+    int32_t i = 1;
+    while (i < n && i < TABLE_MAX && mods[i].fmt == mods[0].fmt) ++i;
+    return i;
+}
+
+/* Places a run's projections: blocks, parts and partial inner vectors; the bytes of the latter. */
+static size_t place(const wsr_lora* mods, int32_t n, int32_t n_tokens, LoraMod* out, char* ws) {
+    const int span = span_of(mods, n, n_tokens);
+    int64_t block = 0;
+    size_t bytes = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        const wsr_lora& m = mods[i];
+        const int64_t last = block + blocks_of(m) - 1;
+        const int pitch = (m.rank + 7) / 8 * 8, parts = (int)(last / span - block / span + 1);
+        if (out)
+            out[i] = LoraMod{m.a, m.b, m.x, m.y0, m.y, reinterpret_cast<float*>(ws + bytes), m.a_stride, m.b_stride,
+                             m.x_tok_stride, m.y0_tok_stride, m.y_tok_stride, m.M, m.K, m.rank, pitch, parts, (int32_t)block};
+        bytes += up256((size_t)parts * n_tokens * pitch * 4);
+        block = last + 1;
+    }
+    return bytes;
 }
 
 size_t lora_workspace(const wsr_lora* mods, int32_t n, int32_t n_tokens) {
-    size_t bytes = lists_bytes(n_tokens);
-    for (int32_t i = 0; i < n; ++i) {
-        int parts, part_k;
-        part_of(mods[i], n, n_tokens, parts, part_k);
-        bytes += up256((size_t)parts * n_tokens * ((mods[i].rank + 15) / 16 * 16) * 4);
+    size_t most = 256;                         /* the runs follow one another and share it */
+    for (int32_t i = 0; i < n;) {
+        const int32_t k = run_of(mods + i, n - i);
+        most = std::max(most, place(mods + i, k, n_tokens, nullptr, nullptr));
+        i += k;
     }
-    return std::max<size_t>(bytes, 256);
+    return order_bytes(n_tokens) + most;
 }
 
-template <int FMT, int NT, int N>
-static hipError_t launch_pair(const LoraTable<N>& tab0, const LoraCall& c, hipStream_t s) {
-    LoraTable<N> tab = tab0;
-    int64_t blocks = 0;
+/* Workgroups of a launch: one per unit and tile, or as many as the chip holds at a time, each with an equal
+   share. */
+static unsigned grid_of(int64_t units, int64_t tiles, int64_t held) {
+    return (unsigned)(tiles * std::max<int64_t>(1, std::min(units, held / tiles)));
+}
+
+template <int FMT, int TT, int RW, int N>
+static hipError_t launch_expand(LoraTable<N>& tab, const LoraCall& c, hipStream_t s) {
+    constexpr int ROWS = LW * 16 * RW;
+    int64_t units = 0;
     for (int i = 0; i < tab.n; ++i) {
-        tab.first[i] = (int32_t)blocks;
-        blocks += (int64_t)tab.mod[i].parts * ((tab.mod[i].rank + RANKS - 1) / RANKS) * c.tile_slots;
+        tab.first[i] = (int32_t)units;
+        units += (tab.mod[i].M + ROWS - 1) / ROWS;
+        if (units > INT32_MAX) return hipErrorInvalidValue;
     }
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_lora_shrink<FMT, NT, N>), dim3((unsigned)blocks), dim3(LT), 0, s, tab, c);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    blocks = 0;
-    for (int i = 0; i < tab.n; ++i) {
-        tab.first[i] = (int32_t)blocks;
-        blocks += (tab.mod[i].M + EXPAND_ROWS - 1) / EXPAND_ROWS * c.tile_slots;
-    }
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_lora_expand<FMT, NT, N>), dim3((unsigned)blocks), dim3(LT), 0, s, tab, c);
+    if (units == 0) return hipSuccess;
+    tab.units = (int32_t)units;
+    hipLaunchKernelGGL((k_lora_expand<FMT, TT, RW, N>), dim3(grid_of(units, c.tiles, EXPAND_HELD)), dim3(LT), 0, s, tab, c);
     return hipGetLastError();
+}
+
+template <int FMT, int TT, int N>
+static hipError_t launch_pair(LoraTable<N>& tab, LoraCall c, hipStream_t s) {
+    int64_t blocks = 0, rows = 0, rank = 0;
+    for (int i = 0; i < tab.n; ++i) {
+        blocks = tab.mod[i].block0 + std::max<int64_t>(1, (tab.mod[i].K + BLOCK_K - 1) / BLOCK_K);
+        tab.first[i] = tab.mod[i].block0;
+        rows += tab.mod[i].M;
+        rank = std::max<int64_t>(rank, tab.mod[i].rank);
+    }
+    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    tab.units = (int32_t)blocks;
+    /* chunks that a tile can have: rounds of RT 16-row tiles, two chunks each, taken by as many workgroups as
+       fill the chip.  One tile for a single adapter of 16 ranks (7.4 us with four, so 6.0) */
+    const int64_t chunks = std::min<int64_t>(std::min(16 * TT, c.n_tokens), std::max(1, c.n_adapters)) *
+                           ((std::min<int64_t>(rank, WINDOW) + 7) / 8);
+    const bool one = TT == 1 && chunks <= 2;
+    const int64_t most = one ? 1 : (chunks + 7) / 8;
+    const int64_t spans = (blocks + c.span - 1) / c.span;
+    c.slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, SHRINK_HELD / (spans * c.tiles)));
+    if (spans * c.tiles * c.slots > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(spans * c.tiles * c.slots));
+    if (one) hipLaunchKernelGGL((k_lora_shrink<FMT, 1, 1, N>), grid, dim3(LT), 0, s, tab, c);
+    else hipLaunchKernelGGL((k_lora_shrink<FMT, TT, 4, N>), grid, dim3(LT), 0, s, tab, c);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    /* few rows: 64 of them per workgroup instead of 256, so that they spread over the chip */
+    if (TT == 1 && rows < 256 * 512) return launch_expand<FMT, 1, 1, N>(tab, c, s);
+    return launch_expand<FMT, TT, 4, N>(tab, c, s);
 }
 
 template <int N>
@@ -349,45 +688,34 @@ static hipError_t launch_table(const LoraMod* mods, int n, int fmt, const LoraCa
     LoraTable<N> tab;
     tab.n = n;
     std::copy(mods, mods + n, tab.mod);
-    const bool one = !c.tiles;
+    const bool one = c.n_tokens <= 16;
     if (fmt == WSR_F16) return one ? launch_pair<WSR_F16, 1, N>(tab, c, s) : launch_pair<WSR_F16, 4, N>(tab, c, s);
     return one ? launch_pair<WSR_BF16, 1, N>(tab, c, s) : launch_pair<WSR_BF16, 4, N>(tab, c, s);
 }
-
-constexpr int TABLE_MAX = 224;
 
 hipError_t launch_lora(const wsr_lora* mods, int32_t n, int32_t n_tokens, const int32_t* adapter_of, int32_t n_adapters,
                        const int32_t* ranks, const float* scales, void* ws, hipStream_t s) {
     char* at = static_cast<char*>(ws);
     LoraCall c{};
     c.adapter_of = adapter_of, c.ranks = ranks, c.scales = scales, c.n_tokens = n_tokens, c.n_adapters = n_adapters;
-    c.tile_slots = (int32_t)most_tiles(n_tokens, n_adapters);
-    if (n_tokens > BALLOT_TOKENS) {
-        int32_t* tiles = reinterpret_cast<int32_t*>(at);
-        int32_t* order = reinterpret_cast<int32_t*>(at + up256(4 * (1 + 3 * (size_t)most_tiles(n_tokens, MAX_ADAPTERS))));
-        at += lists_bytes(n_tokens);
-        c.tiles = tiles, c.order = order;
+    c.tiles = tiles_of(n_tokens);
+    if (n_tokens > TILE) {
+        int32_t* order = reinterpret_cast<int32_t*>(at);
+        at += order_bytes(n_tokens);
+        c.order = order;
         hipLaunchKernelGGL(k_lora_sort, dim3(1), dim3(SORT_THREADS), 4 * ((size_t)n_adapters + 1), s, adapter_of, n_tokens,
-                           n_adapters, tile_cols(n_tokens), tiles, order);
+                           n_adapters, order);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    /* runs of projections of one type, at most a table's length */
     LoraMod run[TABLE_MAX];
-    int held = 0;
-    for (int32_t i = 0; i < n; ++i) {
-        const wsr_lora& m = mods[i];
-        LoraMod d{m.a, m.b, m.x, m.y0, m.y, reinterpret_cast<float*>(at), m.a_stride, m.b_stride, m.x_tok_stride,
-                  m.y0_tok_stride, m.y_tok_stride, m.M, m.K, m.rank, (m.rank + 15) / 16 * 16, 1, 0};
-        part_of(m, n, n_tokens, d.parts, d.part_k);
-        at += up256((size_t)d.parts * n_tokens * d.pitch * 4);
-        run[held++] = d;
-        if (held == TABLE_MAX || i + 1 == n || mods[i + 1].fmt != m.fmt) {
-            const hipError_t e = held <= 8 ? launch_table<8>(run, held, m.fmt, c, s)
-                                           : launch_table<TABLE_MAX>(run, held, m.fmt, c, s);
-            if (e != hipSuccess) return e;
-            held = 0;
-        }
+    for (int32_t i = 0; i < n;) {
+        const int32_t k = run_of(mods + i, n - i);
+        place(mods + i, k, n_tokens, run, at);
+        c.span = span_of(mods + i, k, n_tokens);
+        const hipError_t e = k <= 8 ? launch_table<8>(run, k, mods[i].fmt, c, s) : launch_table<TABLE_MAX>(run, k, mods[i].fmt, c, s);
+        if (e != hipSuccess) return e;
+        i += k;
     }
     return hipSuccess;
 }

@@ -154,3 +154,47 @@ def test_graph_replay_with_other_adapters():
             first = [m["y"].clone() for m in c.mods]
             c.run()
             assert all(torch.equal(f, m["y"]) for f, m in zip(first, c.mods))
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,n,rank", [(8, 4, 16), (40, 5, 8), (150, 30, 12), (20, 3, 96)])
+def test_broken_adapter_reaches_its_own_tokens_only(T, n, rank, dt):
+    """Infinities and NaN in one adapter's weights, and in one token's activations, leave the others' results alone."""
+    c = Case([(130, 128), (64, 72)], T, n, rank, dt, seed=10)
+    c.ids[:n] = torch.arange(n, dtype=torch.int32)
+    c.ids[n + 1] = -1
+    for m in c.mods:
+        m["b"][1, ::3, 0], m["b"][1, 1::3, rank - 1], m["a"][2, 1, 5] = float("nan"), float("inf"), float("inf")
+        m["x"][0, 3] = float("nan")
+    c.run()
+    whole = torch.ones(T, dtype=torch.bool, device="cuda")
+    whole[0] = False
+    whole &= (c.ids != 1) & (c.ids != 2)
+    assert whole.sum() > 0
+    for m in c.mods:
+        y, mag = su.lora64(m["x"], m["a"], m["b"], c.ids.tolist(), None, c.scales.tolist(), m["src"])
+        bound = su.U32 * (8 + 2 * math.sqrt(m["K"]) + 2 * math.sqrt(rank)) * mag
+        assert ((m["y"].double() - y).abs() <= bound)[whole].all()
+        assert torch.isfinite(m["y"][whole]).all() and not torch.isfinite(m["y"][0]).any()
+        assert not torch.isfinite(m["y"][c.ids == 1][:, ::3]).any() and not torch.isfinite(m["y"][c.ids == 2]).any()
+
+
+def test_steady_bits():
+    """The order of tokens inside an adapter's tiles is free; the results are not."""
+    c = Case([(136, 264)], 500, 3, 16, torch.bfloat16, seed=11)
+    c.run()
+    want = c.mods[0]["y"].clone()
+    for _ in range(3):
+        c.mods[0]["y"].fill_(float("nan"))
+        c.run()
+        assert torch.equal(c.mods[0]["y"], want)
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-12, 1e6])
+def test_inner_vectors_of_any_size(size):
+    """f16 activations and weights give inner vectors far from 1: their terms are scaled, not cut."""
+    c = Case([(96, 64)], 5, 2, 16, torch.float16, seed=12, y0="none")
+    c.mods[0]["a"].mul_(min(size, 1.0) ** 0.25 if size < 1 else 30.0)
+    c.mods[0]["x"].mul_(min(size, 1.0) ** 0.15 if size < 1 else 300.0)
+    c.run()
+    c.check()
