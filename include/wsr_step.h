@@ -112,7 +112,8 @@ wsr_status wsr_lora_sweep(const wsr_lora* mods, int32_t n, int32_t n_tokens, con
    are fp32, probabilities are rounded to `fmt` for the product with the values, out once to `fmt`.
    Keys past lens[b] are never read into a result (they may hold anything).
    starts: device int32 [n_seqs + 1], not decreasing, starts[n_seqs] <= n_tokens; lens: device int32
-   [n_seqs], clamped to [0, max_len].  head_dim 64 or 128; every pointer 16-byte aligned and every
+   [n_seqs], clamped to [0, max_len].  prefix_len and max_len at
+   most 2^30.  head_dim 64 or 128; every pointer 16-byte aligned and every
    stride a multiple of 16 (of 4 for lse); tok strides of keys at most 16 MiB; lse (n_tokens, n_heads)
    or null.  k_prefix and v_prefix (k and v) have the same strides.  ws: wsr_attn_workspace_bytes(),
    256-byte aligned. */

@@ -11,7 +11,7 @@
  *         V's transpose comes out of LDS by transposing reads (ds_read_b64_tr_b16).
  *
  * Keys and values go from memory straight into LDS, two buffers, the next block in flight while one is
- * worked on; 16-byte pieces are placed at (piece ^ row) so that reads meet no bank twice.
+ * worked on; 16-byte pieces are placed so that reads meet no bank twice.
  *
  *  - split form (few rows): workgroups over parts of the prefix for all rows, and over parts of each
  *    sequence's own keys; each leaves a maximum, a sum and an unnormalised fp32 row, which
@@ -22,6 +22,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "wsr_step_device.h"
 
@@ -34,7 +35,7 @@ constexpr float A_LOG2E = 1.4426950408889634f;
 struct AttnPlan {
     int32_t prefix_tiles, prefix_parts;    /* row tiles and key parts of the prefix (split form) */
     int32_t own_tiles, own_parts;          /* most row tiles over all sequences, most key parts of one */
-    int64_t prefix_part, own_part;         /* keys of a part */
+    int32_t prefix_part, own_part;         /* keys of a part */
     float* part;                           /* [(prefix_parts + own_parts)][n_tokens][n_heads][head_dim + 2] */
     bool whole;
 };
@@ -43,10 +44,7 @@ struct AttnPlan {
 __device__ __forceinline__ int start_of(const wsr_attn& p, int b) {
     return p.starts ? min(max(p.starts[b], 0), p.n_tokens) : min(b, p.n_tokens);
 }
-__device__ __forceinline__ int64_t len_of(const wsr_attn& p, int b) {
-    const int64_t n = p.lens[b];
-    return n < 0 ? 0 : n > p.max_len ? p.max_len : n;
-}
+__device__ __forceinline__ int len_of(const wsr_attn& p, int b) { return min(max(p.lens[b], 0), (int)p.max_len); }
 
 /* Row tile `tile` of `rows` rows over the sequences: its sequence and its first row there. */
 __device__ __forceinline__ bool find_rows(const wsr_attn& p, int G, int rows, int tile, int& seq, int& row0) {
@@ -74,24 +72,48 @@ __device__ __forceinline__ bool find_rows(const wsr_attn& p, int G, int rows, in
     return false;
 }
 
+typedef __attribute__((address_space(3))) u32x4 l_u32x4;
+typedef __attribute__((address_space(3))) char l_char;
+typedef __attribute__((address_space(3))) s4_t l_s4;
+
+/* The running maximum is only moved when a row's scores pass it by 2^LAZY: until then its probabilities are
+   taken against the old one (at most 2^LAZY, exact after the division by their sum), and the sums and
+   outputs need no rescaling. */
+constexpr float LAZY = 8.f;
+
 /* A workgroup's place: RW waves side by side over rows (32 each), KW = 4 / RW groups of them over
    alternate blocks of KT keys. */
 template <int FMT, int D, int RW>
 struct Attend {
     static constexpr int KW = AW / RW, KT = KW == 1 ? 64 : 32, TILES = KT / 32;
     static constexpr int PIECES = D / 8;                        /* 16-byte pieces of a key */
+    static constexpr int ROW = 2 * D;                           /* bytes of a key */
     static constexpr int HALF = KT * PIECES;                    /* pieces of a block of keys (and of values) */
+    static constexpr int BUFFER = 2 * HALF * 16;                /* bytes of one of a group's two buffers */
     static constexpr int LOADS = HALF / WAVE / RW;              /* of 64 pieces, per wave and plane */
-    static constexpr int DT = D / 32;
+    static constexpr int DT = D / 32, KS = D / 16;
     static constexpr int LDS = KW * 2 * 2 * HALF;               /* pieces of the workgroup */
 
-    u32x4 q[D / 16];
+    u32x4 q[KS];
     f16v_t o[DT];
-    float m, l;                                                 /* the row's maximum; this half's sum */
+    float m, l;                                                 /* the maximum that probabilities are taken against; this half's sum */
+    uint32_t ka[KS], va[DT], koff[LOADS], voff[LOADS];          /* a lane's places in LDS and in a block in memory */
 
-    static __device__ __forceinline__ int swz(int key) { return key & (PIECES - 1); }
+    /* Piece x of a key lies at x ^ swz: the 16 keys of a read of keys, and the four keys times four pieces of a
+       transposing read of values, lie on the 64 banks once each (two keys of 64 share a round of banks). */
+    static __device__ __forceinline__ int kswz(int key) { return D == 128 ? key & 15 : key >> 1 & 7; }
+    static __device__ __forceinline__ int vswz(int key) {
+        return D == 128 ? (key & 3) << 2 | (key >> 2 & 1) : (key >> 1 & 1) << 2 | (key >> 2 & 1);
+    }
 
-    __device__ __forceinline__ void clear() {
+    /* Places relative to the first group's first buffer, `base` bytes on for the wave's own group. */
+    __device__ __forceinline__ void init(uint32_t base, int lane) {
+        const int col = lane % 32, h = lane / 32, r = lane % 16 / 4, c = 2 * (col / 16) + lane % 4 / 2;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) ka[k] = base + col * ROW + ((2 * k + h) ^ kswz(col)) * 16;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+            va[i] = base + HALF * 16 + (4 * h + r) * ROW + ((4 * i + c) ^ vswz(4 * h + r)) * 16 + lane % 2 * 8;
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
@@ -101,57 +123,92 @@ struct Attend {
 
     /* A block of keys and values (rows k0 .. of kb, vb, those from k1 on replaced by the last before it) into a
        buffer of the group. */
-    static __device__ __forceinline__ void fetch(const char* kb, const char* vb, int64_t stride, int64_t k0, int64_t k1,
-                                                 u32x4* buf, int rwave, int lane) {
-        const wsr::rsrc_t kr = wsr::buffer_of(wsr::uniform_ptr(kb + k0 * stride));
-        const wsr::rsrc_t vr = wsr::buffer_of(wsr::uniform_ptr(vb + k0 * stride));
-        const int most = (int)min((int64_t)KT, k1 - k0) - 1;
+    __device__ __forceinline__ void fetch(const char* kb, const char* vb, int64_t stride, int k0, int k1, l_char* buf, int rwave,
+                                          int lane) const {
+        const wsr::rsrc_t kr = wsr::buffer_of(kb + k0 * stride), vr = wsr::buffer_of(vb + k0 * stride);
+        const int most = min(KT, k1 - k0) - 1;
+        if (most == KT - 1) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int at = (rwave * LOADS + i) * WAVE, key = (at + lane) / PIECES, piece = (at + lane) % PIECES;
-            const uint32_t off = (uint32_t)min(key, most) * (uint32_t)stride + 16 * (piece ^ swz(key));
-            wsr::buf_to_lds(kr, buf + at, off, 0);
-            wsr::buf_to_lds(vr, buf + HALF + at, off, 0);
+            for (int i = 0; i < LOADS; ++i) {
+                const int at = (rwave * LOADS + i) * WAVE;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, buf + at * 16, 16, koff[i], 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, buf + (HALF + at) * 16, 16, voff[i], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int at = (rwave * LOADS + i) * WAVE, key = (at + lane) / PIECES, piece = (at + lane) % PIECES;
+                const uint32_t row = (uint32_t)min(key, most) * (uint32_t)stride;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, buf + at * 16, 16, row + 16 * (piece ^ kswz(key)), 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, buf + (HALF + at) * 16, 16, row + 16 * (piece ^ vswz(key)), 0, 0, 0);
+            }
         }
     }
 
-    /* One block of keys: `left` keys of it are visible to this lane's row. */
-    __device__ __forceinline__ void step(const u32x4* buf, int left, bool masked, float c, int lane) {
-        const int col = lane % 32, h = lane / 32;
+    /* One block of keys in buffer `buf` (of the first group): `left` keys of it are visible to this lane's row. */
+    __device__ __forceinline__ void step(const l_char* buf, int left, bool masked, float c, int lane) {
+        const int h = lane / 32;
         f16v_t s[TILES];
+        u32x4 kf[TILES][KS];
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+                kf[t][k] = *(const l_u32x4*)(buf + ka[k] + 32 * t * ROW);
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) s[t][j] = 0.f;
-            const int key = 32 * t + col;
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-                s[t] = mma_32x32x16<FMT>(buf[key * PIECES + ((2 * k + h) ^ swz(key))], q[k], s[t]);
+            for (int k = 0; k < KS; ++k) s[t] = mma_32x32x16<FMT>(kf[t][k], q[k], s[t]);
         }
+        /* KS reads ahead of the products, then one read after each */
+        __builtin_amdgcn_sched_group_barrier(0x100, KS, 0);
+#pragma unroll
+        for (int i = 0; i < (TILES - 1) * KS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, KS, 0);
+        /* values of 16 keys at a time, the next 16 in flight */
+        u32x4 vf[2][DT];
+        auto values = [&](u32x4 (&f)[DT], int t, int k) {
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const u32x2 w = __builtin_bit_cast(
+                        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((l_s4*)(buf + va[i] + (32 * t + 16 * k + 8 * e) * ROW)));
+                    f[i][2 * e] = w.x, f[i][2 * e + 1] = w.y;
+                }
+        };
+        __builtin_amdgcn_sched_barrier(0);
+        values(vf[0], 0, 0);
         if (masked) {
+            asm volatile("");                                   /* a branch: without it every block pays for the selects */
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
                     if (32 * t + 8 * (j / 4) + 4 * h + j % 4 >= left) s[t][j] = A_NEG_INF;
         }
-        float top = m;
+        float top = s[0][0];
 #pragma unroll
         for (int t = 0; t < TILES; ++t)
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[t][j]);
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float base = top == A_NEG_INF ? 0.f : top * c;
-        if (__ballot(top != m)) {
-            const float f = __builtin_amdgcn_exp2f(m * c - base);
+        /* (top - m) c > LAZY, true too where m is -inf and top is not */
+        if (__ballot((top - m) * c > LAZY)) {
+            const float next = fmaxf(m, top), f = next == A_NEG_INF ? 1.f : __builtin_amdgcn_exp2f((m - next) * c);
             l *= f;
 #pragma unroll
             for (int i = 0; i < DT; ++i)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) o[i][j] *= f;
-            m = top;
+            m = next;
         }
-        const char* v = (const char*)(buf + HALF);
+        const float base = m == A_NEG_INF ? 0.f : m * c;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
 #pragma unroll
@@ -161,46 +218,50 @@ struct Attend {
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {                       /* 16 keys */
+                if (t + 1 < TILES || k == 0) values(vf[(k + 1) & 1], k == 0 ? t : t + 1, (k + 1) & 1);
                 u32x4 pt;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) pt[j] = pack2<FMT>(s[t][8 * k + 2 * j], s[t][8 * k + 2 * j + 1]);
 #pragma unroll
-                for (int i = 0; i < DT; ++i) {
-                    u32x4 vt;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int key = 32 * t + 16 * k + 8 * e + 4 * h + lane % 16 / 4;
-                        const int d = 32 * i + 16 * (col / 16) + 4 * (lane % 4);
-                        const char* at = v + (key * PIECES + (d / 8 ^ swz(key))) * 16 + d % 8 * 2;
-                        const u32x2 w = __builtin_bit_cast(
-                            u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4_t*)at));
-                        vt[2 * e] = w.x, vt[2 * e + 1] = w.y;
-                    }
-                    o[i] = mma_32x32x16<FMT>(vt, pt, o[i]);
-                }
+                for (int i = 0; i < DT; ++i) o[i] = mma_32x32x16<FMT>(vf[k][i], pt, o[i]);
             }
         }
     }
 
+    /* Fetches a block into `next` and works on the one in `cur`.  The two pointers are declared not to alias, so
+       that the compiler does not wait for the loads into `next` before it reads `cur`. */
+    __device__ __forceinline__ void round(const l_char* __restrict cur, l_char* __restrict next, uint32_t group_at, const char* kb,
+                                          const char* vb, int64_t stride, int at, int k1, int lim, int low, int high, float c,
+                                          int rwave, int lane) {
+        if (at + KW * KT < k1) fetch(kb, vb, stride, at + KW * KT, k1, next + group_at, rwave, lane);
+        const int end = min(at + KT, k1);
+        if (at < min(end, high)) step(cur, min(lim, end) - at, min(low, end) < at + KT, c, lane);
+    }
+
     /* Keys k0 .. k1 - 1; this lane's row sees those before `lim`, all rows of the wave those before `low`
        and none from `high` on.  Every wave of the workgroup takes part. */
-    __device__ __forceinline__ void walk(const char* kb, const char* vb, int64_t stride, int64_t k0, int64_t k1, int64_t lim,
-                                         int64_t low, int64_t high, float c, u32x4* lds, int wave, int lane) {
+    __device__ __forceinline__ void walk(const char* kb, const char* vb, int64_t stride, int k0, int k1, int lim, int low,
+                                         int high, float c, l_char* lds, int wave, int lane) {
         const int rwave = wave % RW, group = wave / RW;
-        u32x4* mine = lds + group * 4 * HALF;
-        const int64_t rounds = (k1 - k0 + KW * KT - 1) / (KW * KT);
-        int64_t at = k0 + group * KT;
-        if (at < k1) fetch(kb, vb, stride, at, k1, mine, rwave, lane);
-        for (int64_t r = 0; r < rounds; ++r, at += KW * KT) {
+        const uint32_t group_at = group * 2 * BUFFER;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = (rwave * LOADS + i) * WAVE, key = (at + lane) / PIECES, piece = (at + lane) % PIECES;
+            koff[i] = (uint32_t)key * (uint32_t)stride + 16 * (piece ^ kswz(key));
+            voff[i] = (uint32_t)key * (uint32_t)stride + 16 * (piece ^ vswz(key));
+        }
+        int at = k0 + group * KT;
+        if (at < k1) fetch(kb, vb, stride, at, k1, lds + group_at, rwave, lane);
+        for (int left = (k1 - k0 + KW * KT - 1) / (KW * KT); left > 0; left -= 2) {
             wait_loads<0>();
-            __syncthreads();                                    /* block r is in LDS, block r - 1 is done with */
-            const int64_t next = at + KW * KT;
-            if (next < k1) fetch(kb, vb, stride, next, k1, mine + ((r + 1) & 1) * 2 * HALF, rwave, lane);
-            const int64_t end = min(at + KT, k1);
-            if (at < end && at < high) {
-                const int64_t left = lim < end ? lim - at : end - at;
-                step(mine + (r & 1) * 2 * HALF, (int)max(left, (int64_t)-1), low < at + KT || end < at + KT, c, lane);
-            }
+            __syncthreads();                                    /* this block is in LDS, the one before is done with */
+            round(lds, lds + BUFFER, group_at, kb, vb, stride, at, k1, lim, low, high, c, rwave, lane);
+            at += KW * KT;
+            if (left == 1) break;
+            wait_loads<0>();
+            __syncthreads();
+            round(lds + BUFFER, lds, group_at, kb, vb, stride, at, k1, lim, low, high, c, rwave, lane);
+            at += KW * KT;
         }
         __syncthreads();
     }
@@ -243,7 +304,7 @@ struct Attend {
 /* The split form: workgroups below prefix_items take (key head, row tile, part) of the prefix, the others
    (key head, row tile, part) of a sequence's own keys; or, whole, both for a row tile of one sequence. */
 template <int FMT, int D, int RW, bool WHOLE>
-__global__ __launch_bounds__(AT) __attribute__((amdgpu_waves_per_eu(1)))
+__global__ __launch_bounds__(AT) __attribute__((amdgpu_waves_per_eu(RW == 1 ? 1 : 2)))
 void k_attn(wsr_attn p, AttnPlan pl) {
     typedef Attend<FMT, D, RW> A;
     __shared__ u32x4 lds[A::LDS];
@@ -262,21 +323,22 @@ void k_attn(wsr_attn p, AttnPlan pl) {
         if (!WHOLE) item -= pl.prefix_tiles * pl.prefix_parts;
         part = WHOLE ? 0 : item / pl.own_tiles;
         if (!find_rows(p, G, ROWS, WHOLE ? item : item % pl.own_tiles, seq, row0)) return;
-        t0 = start_of(p, seq);
-        rows = (start_of(p, seq + 1) - t0) * G;
+        t0 = __builtin_amdgcn_readfirstlane(start_of(p, seq));
+        rows = __builtin_amdgcn_readfirstlane((start_of(p, seq + 1) - t0) * G);
     }
-    const int64_t own = prefix ? 0 : len_of(p, seq);
-    int64_t k0 = 0, k1 = 0;
+    const int own = prefix ? 0 : __builtin_amdgcn_readfirstlane(len_of(p, seq)), shared = (int)p.prefix_len;
+    int k0 = 0, k1 = 0;
     if (!WHOLE) {
-        k0 = part * (prefix ? pl.prefix_part : pl.own_part);
-        k1 = min(k0 + (prefix ? pl.prefix_part : pl.own_part), prefix ? p.prefix_len : own);
-        if (k0 >= k1) return;
+        const int keys = prefix ? pl.prefix_part : pl.own_part, all = prefix ? shared : own;
+        if ((int64_t)part * keys >= all) return;
+        k0 = part * keys;
+        k1 = all - k0 > keys ? k0 + keys : all;
     }
     const int row = row0 + rwave * 32 + col;                    /* this lane's row, both halves the same */
     const bool valid = row < rows;
-    const int tok = t0 + min(row, rows - 1) / G, qh = head * G + min(row, rows - 1) % G;
+    const int at_row = min(row, rows - 1) / G, tok = t0 + at_row, qh = head * G + min(row, rows - 1) - at_row * G;
     A a;
-    a.clear();
+    a.init(wave / RW * 2 * A::BUFFER, lane);
     {
         const char* qr = (const char*)p.q + tok * p.q_tok_stride + qh * p.q_head_stride;
 #pragma unroll
@@ -285,23 +347,21 @@ void k_attn(wsr_attn p, AttnPlan pl) {
     const float c = p.scale * A_LOG2E;
     const bool busy = row0 + rwave * 32 < rows;                 /* the wave has rows */
     if (WHOLE || prefix) {
-        const int64_t e = WHOLE ? p.prefix_len : k1;
+        const int e = WHOLE ? shared : k1;
         if (e > k0)
             a.walk((const char*)p.k_prefix + head * p.prefix_head_stride, (const char*)p.v_prefix + head * p.prefix_head_stride,
-                   p.prefix_tok_stride, k0, e, e, e, busy ? e : 0, c, lds, wave, lane);
+                   p.prefix_tok_stride, k0, e, e, e, busy ? e : 0, c, (l_char*)lds, wave, lane);
     }
     if (WHOLE || !prefix) {
         /* row i of the sequence's n: keys before own - n + i + 1 */
-        const int n = rows / G;
-        const int64_t lim = own - n + min(row, rows - 1) / G + 1;
-        const int64_t low = own - n + min(row0 + rwave * 32, rows - 1) / G + 1;
-        const int64_t high = busy ? own - n + min(row0 + rwave * 32 + 31, rows - 1) / G + 1 : 0;
-        const int64_t last = own - n + min(row0 + ROWS - 1, rows - 1) / G + 1;   /* of the workgroup's rows */
-        const int64_t e = min(WHOLE ? own : k1, last);
+        const int past = own - rows / G + 1;
+        const int low = past + min(row0 + rwave * 32, rows - 1) / G;
+        const int high = busy ? past + min(row0 + rwave * 32 + 31, rows - 1) / G : 0;
+        const int e = min(WHOLE ? own : k1, past + min(row0 + ROWS - 1, rows - 1) / G);   /* of the workgroup's rows */
         if (e > k0)
             a.walk((const char*)p.k + seq * p.kv_seq_stride + head * p.kv_head_stride,
-                   (const char*)p.v + seq * p.kv_seq_stride + head * p.kv_head_stride, p.kv_tok_stride, k0, e, lim, low,
-                   high, c, lds, wave, lane);
+                   (const char*)p.v + seq * p.kv_seq_stride + head * p.kv_head_stride, p.kv_tok_stride, k0, e, past + at_row,
+                   low, high, c, (l_char*)lds, wave, lane);
     }
     a.join(lds, c, wave, lane);
     if (wave >= RW || !valid) return;
@@ -348,8 +408,8 @@ __global__ __launch_bounds__(AT) void k_attn_join(wsr_attn p, AttnPlan pl) {
     int own = 0;
     if (seq >= 0 && tok < start_of(p, seq + 1)) {
         /* own keys that the token sees */
-        const int64_t seen = min(len_of(p, seq), len_of(p, seq) - (start_of(p, seq + 1) - tok) + 1);
-        if (seen > 0) own = (int)((seen + pl.own_part - 1) / pl.own_part);
+        const int seen = len_of(p, seq) - (start_of(p, seq + 1) - tok) + 1;
+        if (seen > 0) own = (seen - 1) / pl.own_part + 1;
     }
     const int n = pl.prefix_parts + own;
     constexpr int E = D / WAVE;
@@ -389,11 +449,10 @@ static AttnPlan attn_plan(const wsr_attn& p) {
     const int64_t tiles = (rows + 32 * rw - 1) / (32 * rw), per = tiles * p.n_kv_heads;
     pl.prefix_tiles = (int32_t)tiles;
     const int64_t block = rw == 4 ? 64 : 64 * (4 / rw);
-    auto parts = [&](int64_t keys, int64_t units, int64_t least, int64_t& part) {
+    auto parts = [&](int64_t keys, int64_t units, int64_t least, int32_t& part) {
         if (keys <= 0) return (int32_t)0;
         const int64_t want = std::max<int64_t>(1, 512 / std::max<int64_t>(1, units));
-        part = std::max(least, (keys + want - 1) / want);
-        part = (part + block - 1) / block * block;
+        part = (int32_t)std::min<int64_t>((std::max(least, (keys + want - 1) / want) + block - 1) / block * block, 1 << 30);
         return (int32_t)((keys + part - 1) / part);
     };
     pl.prefix_parts = parts(p.prefix_len, per, 256, pl.prefix_part);
