@@ -17,7 +17,9 @@
  *    sequence's own keys; each leaves a maximum, a sum and an unnormalised fp32 row, which
  *    k_attn_join adds up.
  *  - whole form (prompts): a workgroup takes 128 rows of one sequence through the prefix and its own
- *    keys and stores the result.
+ *    keys and stores the result.  The chip holds 512 such workgroups at a time; the last round of them,
+ *    where it would leave places empty, is cut into parts along the keys that fill them (a part leaves what
+ *    one of the split form does, and k_attn_join_units adds them up).
  */
 #include <hip/hip_runtime.h>
 
@@ -36,7 +38,9 @@ struct AttnPlan {
     int32_t prefix_tiles, prefix_parts;    /* row tiles and key parts of the prefix (split form) */
     int32_t own_tiles, own_parts;          /* most row tiles over all sequences, most key parts of one */
     int32_t prefix_part, own_part;         /* keys of a part */
-    float* part;                           /* [(prefix_parts + own_parts)][n_tokens][n_heads][head_dim + 2] */
+    int32_t most_parts;                    /* parts of a unit of the whole form's last round, at most */
+    float* part;                           /* [(prefix_parts + own_parts)][n_tokens][n_heads][head_dim + 4], or
+                                              whole: [HELD][128][head_dim + 4] */
     bool whole;
 };
 
@@ -46,25 +50,34 @@ __device__ __forceinline__ int start_of(const wsr_attn& p, int b) {
 }
 __device__ __forceinline__ int len_of(const wsr_attn& p, int b) { return min(max(p.lens[b], 0), (int)p.max_len); }
 
-/* Row tile `tile` of `rows` rows over the sequences: its sequence and its first row there. */
-__device__ __forceinline__ bool find_rows(const wsr_attn& p, int G, int rows, int tile, int& seq, int& row0) {
+/* Row tile `tile` of `rows` rows over the sequences: its sequence, first row there, first token, rows of the
+   sequence and its own keys. */
+struct Place {
+    int seq, row0, t0, rows, own;
+};
+__device__ __forceinline__ bool find_rows(const wsr_attn& p, int G, int rows, int tile, Place& o) {
     const int lane = threadIdx.x % WAVE;
     for (int b0 = 0; b0 < p.n_seqs; b0 += WAVE) {
         const int b = b0 + lane;
-        int n = 0;
-        if (b < p.n_seqs) n = (max(start_of(p, b + 1) - start_of(p, b), 0) * G + rows - 1) / rows;
+        int n = 0, first = 0, count = 0, len = 0;
+        if (b < p.n_seqs) {
+            first = start_of(p, b), len = len_of(p, b);
+            count = max(start_of(p, b + 1) - first, 0) * G;
+            n = (count + rows - 1) / rows;
+        }
         int sum = n;                                            /* tiles up to and with this sequence */
 #pragma unroll
         for (int k = 1; k < WAVE; k <<= 1) {
-            const int o = __shfl_up(sum, k);
-            if (lane >= k) sum += o;
+            const int v = __shfl_up(sum, k);
+            if (lane >= k) sum += v;
         }
-        const int all = __shfl(sum, WAVE - 1);
+        const int all = __builtin_amdgcn_readlane(sum, WAVE - 1);
         if (tile < all) {
-            const uint64_t after = __ballot(sum > tile);
-            const int w = __builtin_ctzll(after);
-            seq = __builtin_amdgcn_readfirstlane(b0 + w);
-            row0 = __builtin_amdgcn_readfirstlane((tile - (__shfl(sum, w) - __shfl(n, w))) * rows);
+            const int w = __builtin_ctzll(__ballot(sum > tile));
+            o.seq = b0 + w;
+            o.row0 = (tile - (__builtin_amdgcn_readlane(sum, w) - __builtin_amdgcn_readlane(n, w))) * rows;
+            o.t0 = __builtin_amdgcn_readlane(first, w), o.rows = __builtin_amdgcn_readlane(count, w);
+            o.own = __builtin_amdgcn_readlane(len, w);
             return true;
         }
         tile -= all;
@@ -80,6 +93,27 @@ typedef __attribute__((address_space(3))) s4_t l_s4;
    taken against the old one (at most 2^LAZY, exact after the division by their sum), and the sums and
    outputs need no rescaling. */
 constexpr float LAZY = 8.f;
+
+/* Row tiles over all sequences. */
+__device__ __forceinline__ int count_tiles(const wsr_attn& p, int G, int rows) {
+    int n = 0;
+    for (int b = threadIdx.x % WAVE; b < p.n_seqs; b += WAVE) n += (max(start_of(p, b + 1) - start_of(p, b), 0) * G + rows - 1) / rows;
+#pragma unroll
+    for (int k = 32; k; k >>= 1) n += __shfl_xor(n, k);
+    return __builtin_amdgcn_readfirstlane(n);
+}
+
+/* The units (row tile, key head) of the whole form: the first `full` go to a workgroup each, the other `rest` to
+   `parts` of them each. */
+constexpr int JOIN_ROWS = 4;
+constexpr int HELD = 512;                      /* workgroups on the chip at a time: two per CU */
+struct Round {
+    int full, rest, parts;
+};
+__device__ __forceinline__ Round last_round(const wsr_attn& p, const AttnPlan& pl, int tiles) {
+    const int units = tiles * p.n_kv_heads, rest = units % HELD, parts = rest ? min(pl.most_parts, HELD / rest) : 1;
+    return parts > 1 ? Round{units - rest, rest, parts} : Round{units, 0, 1};
+}
 
 /* A workgroup's place: RW waves side by side over rows (32 each), KW = 4 / RW groups of them over
    alternate blocks of KT keys. */
@@ -162,14 +196,15 @@ struct Attend {
 #pragma unroll
             for (int k = 0; k < KS; ++k) s[t] = mma_32x32x16<FMT>(kf[t][k], q[k], s[t]);
         }
-        /* KS reads ahead of the products, then one read after each */
-        __builtin_amdgcn_sched_group_barrier(0x100, KS, 0);
+        /* AHEAD reads before the products, then one read after each */
+        constexpr int AHEAD = KS < 6 ? KS : 6;
+        __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
-        for (int i = 0; i < (TILES - 1) * KS; ++i) {
+        for (int i = 0; i < TILES * KS - AHEAD; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, KS, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
         /* values of 16 keys at a time, the next 16 in flight */
         u32x4 vf[2][DT];
         auto values = [&](u32x4 (&f)[DT], int t, int k) {
@@ -228,12 +263,25 @@ struct Attend {
         }
     }
 
-    /* Fetches a block into `next` and works on the one in `cur`.  The two pointers are declared not to alias, so
-       that the compiler does not wait for the loads into `next` before it reads `cur`. */
+    /* Blocks alternate between two buffers: a block is fetched while the one before it is worked on.  A wave with
+       buffers of its own needs no barrier and fetches a block before it waits for the one before it, so that two
+       are in flight (one token on 32771 keys, 32 heads on 8: 45 us with barriers, 37 without; groups of two or
+       four waves, which would need a second barrier for it, gained nothing: 96 and 103 us, 59 and 60).
+       The two pointers are declared not to alias, so that the compiler does not wait for the loads into `next`
+       before it reads `cur`. */
+    static constexpr bool DEEP = RW == 1;
     __device__ __forceinline__ void round(const l_char* __restrict cur, l_char* __restrict next, uint32_t group_at, const char* kb,
                                           const char* vb, int64_t stride, int at, int k1, int lim, int low, int high, float c,
                                           int rwave, int lane) {
-        if (at + KW * KT < k1) fetch(kb, vb, stride, at + KW * KT, k1, next + group_at, rwave, lane);
+        const bool more = at + KW * KT < k1;
+        if constexpr (!DEEP) {
+            wait_loads<0>();
+            __syncthreads();                                    /* `cur` is there, `next` has been read */
+            if (more) fetch(kb, vb, stride, at + KW * KT, k1, next + group_at, rwave, lane);
+        } else if (more) {
+            fetch(kb, vb, stride, at + KW * KT, k1, next + group_at, rwave, lane);
+            wait_loads<2 * LOADS>();
+        } else wait_loads<0>();
         const int end = min(at + KT, k1);
         if (at < min(end, high)) step(cur, min(lim, end) - at, min(low, end) < at + KT, c, lane);
     }
@@ -253,13 +301,9 @@ struct Attend {
         int at = k0 + group * KT;
         if (at < k1) fetch(kb, vb, stride, at, k1, lds + group_at, rwave, lane);
         for (int left = (k1 - k0 + KW * KT - 1) / (KW * KT); left > 0; left -= 2) {
-            wait_loads<0>();
-            __syncthreads();                                    /* this block is in LDS, the one before is done with */
             round(lds, lds + BUFFER, group_at, kb, vb, stride, at, k1, lim, low, high, c, rwave, lane);
             at += KW * KT;
             if (left == 1) break;
-            wait_loads<0>();
-            __syncthreads();
             round(lds + BUFFER, lds, group_at, kb, vb, stride, at, k1, lim, low, high, c, rwave, lane);
             at += KW * KT;
         }
@@ -311,27 +355,46 @@ void k_attn(wsr_attn p, AttnPlan pl) {
     constexpr int ROWS = 32 * RW;
     const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), rwave = wave % RW, col = lane % 32;
     const int G = p.n_heads / p.n_kv_heads;
-    const int head = blockIdx.x % p.n_kv_heads;
-    int item = blockIdx.x / p.n_kv_heads;
+    int item = blockIdx.x, part = 0, parts = 1;
+    if (WHOLE) {
+        const Round r = last_round(p, pl, count_tiles(p, G, ROWS));
+        if (item >= r.full) {
+            const int j = item - r.full;
+            if (j >= r.rest * r.parts) return;
+            part = j / r.rest, parts = r.parts, item = r.full + j % r.rest;
+        }
+    }
+    const int head = item % p.n_kv_heads;
+    item /= p.n_kv_heads;
     const bool prefix = !WHOLE && item < pl.prefix_tiles * pl.prefix_parts;
-    int seq = 0, row0, part, t0 = 0, rows;
+    int seq = 0, row0, t0 = 0, rows, own = 0;
     if (prefix) {
         row0 = item % pl.prefix_tiles * ROWS;
         part = item / pl.prefix_tiles;
         rows = p.n_tokens * G;
     } else {
-        if (!WHOLE) item -= pl.prefix_tiles * pl.prefix_parts;
-        part = WHOLE ? 0 : item / pl.own_tiles;
-        if (!find_rows(p, G, ROWS, WHOLE ? item : item % pl.own_tiles, seq, row0)) return;
-        t0 = __builtin_amdgcn_readfirstlane(start_of(p, seq));
-        rows = __builtin_amdgcn_readfirstlane((start_of(p, seq + 1) - t0) * G);
+        if (!WHOLE) {
+            item -= pl.prefix_tiles * pl.prefix_parts;
+            part = item / pl.own_tiles;
+            item %= pl.own_tiles;
+        }
+        Place o;
+        if (!find_rows(p, G, ROWS, item, o)) return;
+        seq = o.seq, row0 = o.row0, t0 = o.t0, rows = o.rows, own = o.own;
     }
-    const int own = prefix ? 0 : __builtin_amdgcn_readfirstlane(len_of(p, seq)), shared = (int)p.prefix_len;
+    const int shared = (int)p.prefix_len;
+    /* rows of a sequence: row i of its n sees own keys before past + i */
+    const int past = own - rows / G + 1;
+    const int seen = max(0, past + min(row0 + ROWS - 1, rows - 1) / G);    /* own keys that a row of the workgroup sees */
     int k0 = 0, k1 = 0;
     if (!WHOLE) {
         const int keys = prefix ? pl.prefix_part : pl.own_part, all = prefix ? shared : own;
         if ((int64_t)part * keys >= all) return;
         k0 = part * keys;
+        k1 = all - k0 > keys ? k0 + keys : all;
+    } else {                                   /* of the prefix and the own keys behind it */
+        const int all = shared + seen, keys = ((all + parts - 1) / parts + A::KT - 1) / A::KT * A::KT;
+        k0 = min(part * keys, all);
         k1 = all - k0 > keys ? k0 + keys : all;
     }
     const int row = row0 + rwave * 32 + col;                    /* this lane's row, both halves the same */
@@ -346,27 +409,22 @@ void k_attn(wsr_attn p, AttnPlan pl) {
     }
     const float c = p.scale * A_LOG2E;
     const bool busy = row0 + rwave * 32 < rows;                 /* the wave has rows */
-    if (WHOLE || prefix) {
-        const int e = WHOLE ? shared : k1;
-        if (e > k0)
-            a.walk((const char*)p.k_prefix + head * p.prefix_head_stride, (const char*)p.v_prefix + head * p.prefix_head_stride,
-                   p.prefix_tok_stride, k0, e, e, e, busy ? e : 0, c, (l_char*)lds, wave, lane);
-    }
-    if (WHOLE || !prefix) {
-        /* row i of the sequence's n: keys before own - n + i + 1 */
-        const int past = own - rows / G + 1;
-        const int low = past + min(row0 + rwave * 32, rows - 1) / G;
-        const int high = busy ? past + min(row0 + rwave * 32 + 31, rows - 1) / G : 0;
-        const int e = min(WHOLE ? own : k1, past + min(row0 + ROWS - 1, rows - 1) / G);   /* of the workgroup's rows */
-        if (e > k0)
-            a.walk((const char*)p.k + seq * p.kv_seq_stride + head * p.kv_head_stride,
-                   (const char*)p.v + seq * p.kv_seq_stride + head * p.kv_head_stride, p.kv_tok_stride, k0, e, past + at_row,
-                   low, high, c, (l_char*)lds, wave, lane);
+    /* the prefix, then the sequence's own keys: one copy of the loop for both */
+#pragma unroll 1
+    for (int s = WHOLE ? 0 : !prefix; s <= (WHOLE ? 1 : !prefix); ++s) {
+        const int low = s ? past + min(row0 + rwave * 32, rows - 1) / G : k1;
+        const int high = !busy ? 0 : s ? past + min(row0 + rwave * 32 + 31, rows - 1) / G : k1;
+        const int b = WHOLE && s ? max(k0 - shared, 0) : k0;
+        const int e = !s ? min(k1, shared) : WHOLE ? k1 - shared : min(k1, seen);
+        if (e <= b) continue;
+        const int64_t at = s ? seq * p.kv_seq_stride + head * p.kv_head_stride : head * p.prefix_head_stride;
+        a.walk((const char*)(s ? p.k : p.k_prefix) + at, (const char*)(s ? p.v : p.v_prefix) + at,
+               s ? p.kv_tok_stride : p.prefix_tok_stride, b, e, s ? past + at_row : k1, low, high, c, (l_char*)lds, wave, lane);
     }
     a.join(lds, c, wave, lane);
     if (wave >= RW || !valid) return;
     const int h = lane / 32;
-    if (WHOLE) {
+    if (WHOLE && parts == 1) {
         const float inv = a.l > 0.f ? 1.f / a.l : a.l == 0.f ? 0.f : a.l;
         char* out = (char*)p.out + tok * p.out_tok_stride + qh * p.out_head_stride;
 #pragma unroll
@@ -378,7 +436,8 @@ void k_attn(wsr_attn p, AttnPlan pl) {
                           pack2<FMT>(a.o[i][4 * j + 2] * inv, a.o[i][4 * j + 3] * inv)};
         if (p.lse && h == 0) p.lse[(int64_t)tok * p.n_heads + qh] = a.m == A_NEG_INF ? a.m : a.m * p.scale + logf(a.l);
     } else {
-        const int64_t slot = ((int64_t)(prefix ? part : pl.prefix_parts + part) * p.n_tokens + tok) * p.n_heads + qh;
+        const int64_t slot = WHOLE ? (int64_t)(blockIdx.x % HELD) * ROWS + row - row0  /* full is a multiple of HELD */
+                                   : ((int64_t)(prefix ? part : pl.prefix_parts + part) * p.n_tokens + tok) * p.n_heads + qh;
         float* w = pl.part + slot * (D + 4);
 #pragma unroll
         for (int i = 0; i < A::DT; ++i)
@@ -388,6 +447,28 @@ void k_attn(wsr_attn p, AttnPlan pl) {
                     f4_t{a.o[i][4 * j], a.o[i][4 * j + 1], a.o[i][4 * j + 2], a.o[i][4 * j + 3]};
         if (h == 0) w[D] = a.m, w[D + 1] = a.l;
     }
+}
+
+/* Adds up the n parts of a row, `step` floats apart, and stores it, by one wave. */
+template <int FMT, int D>
+__device__ __forceinline__ void join_row(const wsr_attn& p, const float* w, int64_t step, int n, int tok, int qh, int lane) {
+    constexpr int E = D / WAVE;
+    const float c = p.scale * A_LOG2E;
+    float m = A_NEG_INF, l = 0.f, o[E] = {};
+    for (int i = 0; i < n; ++i) {
+        const float* v = w + i * step;
+        const float m2 = v[D], top = fmaxf(m, m2), base = top == A_NEG_INF ? 0.f : top * c;
+        const float a = __builtin_amdgcn_exp2f(m * c - base), b = __builtin_amdgcn_exp2f(m2 * c - base);
+        l = l * a + v[D + 1] * b;
+        m = top;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = o[e] * a + v[E * lane + e] * b;
+    }
+    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+    char* out = (char*)p.out + tok * p.out_tok_stride + qh * p.out_head_stride;
+    if constexpr (E == 2) ((uint32_t*)out)[lane] = pack2<FMT>(o[0] * inv, o[1] * inv);
+    else ((uint16_t*)out)[lane] = (uint16_t)pack2<FMT>(o[0] * inv, 0.f);
+    if (p.lse && lane == 0) p.lse[(int64_t)tok * p.n_heads + qh] = m == A_NEG_INF ? m : m * p.scale + logf(l);
 }
 
 /* One wave per (token, head): the parts that were written, in order. */
@@ -411,65 +492,67 @@ __global__ __launch_bounds__(AT) void k_attn_join(wsr_attn p, AttnPlan pl) {
         const int seen = len_of(p, seq) - (start_of(p, seq + 1) - tok) + 1;
         if (seen > 0) own = (seen - 1) / pl.own_part + 1;
     }
-    const int n = pl.prefix_parts + own;
-    constexpr int E = D / WAVE;
-    const int64_t step = (int64_t)p.n_tokens * p.n_heads * (D + 4);
-    const float* w = pl.part + row * (D + 4);
-    const float c = p.scale * A_LOG2E;
-    float m = A_NEG_INF, l = 0.f, o[E] = {};
-    for (int i = 0; i < n; ++i) {
-        const float* v = w + i * step;
-        const float m2 = v[D], top = fmaxf(m, m2), base = top == A_NEG_INF ? 0.f : top * c;
-        const float a = __builtin_amdgcn_exp2f(m * c - base), b = __builtin_amdgcn_exp2f(m2 * c - base);
-        l = l * a + v[D + 1] * b;
-        m = top;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * a + v[E * lane + e] * b;
+    join_row<FMT, D>(p, pl.part + row * (D + 4), (int64_t)p.n_tokens * p.n_heads * (D + 4), pl.prefix_parts + own, tok, qh, lane);
+}
+
+/* The parts of the whole form's last round: a wave per row of its units. */
+template <int FMT, int D>
+__global__ __launch_bounds__(AT) void k_attn_join_units(wsr_attn p, AttnPlan pl) {
+    constexpr int ROWS = 128;
+    const int G = p.n_heads / p.n_kv_heads, lane = threadIdx.x % WAVE, wave = wsr::wave_in_block();
+    const Round r = last_round(p, pl, count_tiles(p, G, ROWS));
+    for (int i = blockIdx.x; i < r.rest * (ROWS / JOIN_ROWS); i += gridDim.x) {
+        const int unit = i / (ROWS / JOIN_ROWS), item = r.full + unit;
+        Place o;
+        if (!find_rows(p, G, ROWS, item / p.n_kv_heads, o)) return;
+        for (int k = wave; k < JOIN_ROWS; k += AW) {
+            const int at = i % (ROWS / JOIN_ROWS) * JOIN_ROWS + k, row = o.row0 + at;
+            if (row < o.rows)
+                join_row<FMT, D>(p, pl.part + ((int64_t)unit * ROWS + at) * (D + 4), (int64_t)r.rest * ROWS * (D + 4), r.parts,
+                                 o.t0 + row / G, item % p.n_kv_heads * G + row % G, lane);
+        }
     }
-    const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-    char* out = (char*)p.out + tok * p.out_tok_stride + qh * p.out_head_stride;
-    if constexpr (E == 2) ((uint32_t*)out)[lane] = pack2<FMT>(o[0] * inv, o[1] * inv);
-    else ((uint16_t*)out)[lane] = (uint16_t)pack2<FMT>(o[0] * inv, 0.f);
-    if (p.lse && lane == 0) p.lse[row] = m == A_NEG_INF ? m : m * p.scale + logf(l);
 }
 
 /* ---- host ------------------------------------------------------------------------------------------ */
 
-constexpr int64_t WHOLE_TILES = 256;           /* row tiles times key heads from which the whole form is taken */
-
+constexpr int LEAST = 256;                     /* keys of a part */
 static int row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 
 static AttnPlan attn_plan(const wsr_attn& p) {
     AttnPlan pl{};
     const int64_t G = p.n_heads / p.n_kv_heads, rows = p.n_tokens * G;
     const int rw = row_waves(rows);
-    pl.whole = rw == 4 && p.n_kv_heads * (rows / 128) >= WHOLE_TILES && rows >= 64 * (int64_t)p.n_seqs;
+    /* with fewer rows of a sequence most of its row tile would be empty, and with fewer tiles the split form's
+       joining costs less (2 x 300 queries on 2001 keys, 32 heads on 8: 47 us whole, 43 split) */
+    pl.whole = rw == 4 && rows >= 64 * (int64_t)p.n_seqs && p.n_kv_heads * (rows / 128) >= HELD / 2;
+    pl.most_parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(16, (p.prefix_len + p.max_len) / 256));
     pl.own_tiles = (int32_t)(rows / (32 * rw) + std::min<int64_t>(p.n_seqs, p.n_tokens));
     if (pl.whole) return pl;
     const int64_t tiles = (rows + 32 * rw - 1) / (32 * rw), per = tiles * p.n_kv_heads;
     pl.prefix_tiles = (int32_t)tiles;
-    const int64_t block = rw == 4 ? 64 : 64 * (4 / rw);
+    const int64_t block = rw == 4 ? 64 : 32 * (4 / rw), held = rw == 1 ? HELD / 2 : HELD;
     auto parts = [&](int64_t keys, int64_t units, int64_t least, int32_t& part) {
         if (keys <= 0) return (int32_t)0;
-        const int64_t want = std::max<int64_t>(1, 512 / std::max<int64_t>(1, units));
+        const int64_t want = std::max<int64_t>(1, held / std::max<int64_t>(1, units));
         part = (int32_t)std::min<int64_t>((std::max(least, (keys + want - 1) / want) + block - 1) / block * block, 1 << 30);
         return (int32_t)((keys + part - 1) / part);
     };
-    pl.prefix_parts = parts(p.prefix_len, per, 256, pl.prefix_part);
-    pl.own_parts = parts(p.max_len, (int64_t)pl.own_tiles * p.n_kv_heads, 256, pl.own_part);
+    pl.prefix_parts = parts(p.prefix_len, per, LEAST, pl.prefix_part);
+    pl.own_parts = parts(p.max_len, (int64_t)pl.own_tiles * p.n_kv_heads, LEAST, pl.own_part);
     return pl;
 }
 
 size_t attn_workspace(const wsr_attn& p) {
     const AttnPlan pl = attn_plan(p);
-    if (pl.whole) return 256;
+    if (pl.whole) return pl.most_parts > 1 ? (size_t)HELD * 128 * (p.head_dim + 4) * 4 : 256;
     return std::max<size_t>(256, (size_t)(pl.prefix_parts + pl.own_parts) * p.n_tokens * p.n_heads * (p.head_dim + 4) * 4);
 }
 
 template <int FMT, int D>
 static hipError_t launch_dim(const wsr_attn& p, const AttnPlan& pl, hipStream_t s) {
     const int64_t items = pl.whole ? pl.own_tiles : (int64_t)pl.prefix_tiles * pl.prefix_parts + (int64_t)pl.own_tiles * pl.own_parts;
-    const int64_t blocks = items * p.n_kv_heads;
+    const int64_t blocks = items * p.n_kv_heads + (pl.whole && pl.most_parts > 1 ? HELD : 0);
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks), threads(AT);
     if (blocks > 0) {
@@ -480,7 +563,11 @@ static hipError_t launch_dim(const wsr_attn& p, const AttnPlan& pl, hipStream_t 
             default: hipLaunchKernelGGL((k_attn<FMT, D, 4, false>), grid, threads, 0, s, p, pl); break;
         }
         const hipError_t e = hipGetLastError();
-        if (e != hipSuccess || pl.whole) return e;
+        if (e != hipSuccess || (pl.whole && pl.most_parts == 1)) return e;
+    }
+    if (pl.whole) {
+        hipLaunchKernelGGL((k_attn_join_units<FMT, D>), dim3(2048), threads, 0, s, p, pl);
+        return hipGetLastError();
     }
     const int64_t rows = (int64_t)p.n_tokens * p.n_heads;
     hipLaunchKernelGGL((k_attn_join<FMT, D>), dim3((unsigned)((rows + AW - 1) / AW)), threads, 0, s, p, pl);
