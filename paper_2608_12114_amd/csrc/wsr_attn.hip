@@ -232,7 +232,7 @@ struct Attend {
         for (int t = 0; t < TILES; ++t)
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[t][j]);
-        top = fmaxf(top, __shfl_xor(top, 32));
+        top = xchg_max<0>(top);
         /* (top - m) c > LAZY, true too where m is -inf and top is not */
         if (__ballot((top - m) * c > LAZY)) {
             const float next = fmaxf(m, top), f = next == A_NEG_INF ? 1.f : __builtin_amdgcn_exp2f((m - next) * c);
@@ -313,7 +313,7 @@ struct Attend {
     /* Adds up the groups' results in LDS; the first group's waves hold the row's maximum, sum (both halves)
        and output afterwards. */
     __device__ __forceinline__ void join(u32x4* lds, float c, int wave, int lane) {
-        l += __shfl_xor(l, 32);
+        l = wsr::xchg_add<0>(l);
         if constexpr (KW > 1) {
             float* f = (float*)lds;
             constexpr int PER = WAVE * (16 * DT + 2);           /* floats that a wave leaves */

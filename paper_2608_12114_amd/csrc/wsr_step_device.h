@@ -87,11 +87,45 @@ __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int k = 32; k; k >>= 1) v = fmaxf(v, __shfl_xor(v, k));
-    return v;
+/* v combined with its partner lane's v, by the levels of wsr::xchg_add: lane swaps for levels 0 and 1 (halves,
+   then 16-lane rows), moves inside a 16-lane row for levels 2 to 5.  OP must not depend on the order of its
+   operands; applied level by level it leaves the same bits in all lanes. */
+template <int LEVEL>
+__device__ __forceinline__ void partners(uint32_t v, uint32_t& a, uint32_t& b) {
+    if constexpr (LEVEL == 0) {
+        const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        a = s[0], b = s[1];
+    } else if constexpr (LEVEL == 1) {
+        const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        a = s[0], b = s[1];
+    } else {
+        constexpr int CTRL = LEVEL == 2 ? wsr::DPP_MIRROR : LEVEL == 3 ? wsr::DPP_HALF_MIRROR : LEVEL == 4 ? wsr::DPP_XOR2 : wsr::DPP_XOR1;
+        a = v;
+        b = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+    }
 }
+template <int LEVEL>
+__device__ __forceinline__ float xchg_max(float v) {
+    uint32_t a, b;
+    partners<LEVEL>(__float_as_uint(v), a, b);
+    return fmaxf(__uint_as_float(a), __uint_as_float(b));
+}
+template <int LEVEL>
+__device__ __forceinline__ int xchg_min(int v) {
+    uint32_t a, b;
+    partners<LEVEL>((uint32_t)v, a, b);
+    return min((int)a, (int)b);
+}
+
+/* Over a 16-lane row. */
+__device__ __forceinline__ float row_max(float v) { return xchg_max<5>(xchg_max<4>(xchg_max<3>(xchg_max<2>(v)))); }
+__device__ __forceinline__ int row_min(int v) { return xchg_min<5>(xchg_min<4>(xchg_min<3>(xchg_min<2>(v)))); }
+__device__ __forceinline__ float row_sum(float v) {
+    return wsr::xchg_add<5>(wsr::xchg_add<4>(wsr::xchg_add<3>(wsr::xchg_add<2>(v))));
+}
+/* Over a wave. */
+__device__ __forceinline__ float wave_max(float v) { return row_max(xchg_max<1>(xchg_max<0>(v))); }
+__device__ __forceinline__ int wave_min(int v) { return row_min(xchg_min<1>(xchg_min<0>(v))); }
 
 /* D = A B + C on 16 x 16 x 32: lane l holds row l % 16 of A and column l % 16 of B, elements
    8 (l / 16) .. + 7 of their 32; D's column l % 16, rows 4 (l / 16) .. + 3. */

@@ -3,14 +3,14 @@
  * acceptance of each sequence's drafts and the race for its next token.
  *
  *   k_verify_stats   (row, chunk): largest logit, its lowest index and the sum of exponentials, one
- *                    read of the row; chunks of CHUNK logits keep few rows spread over the chip
+ *                    read of the row; chunks keep few rows spread over the chip
  *   k_verify_race    (sequence, chunk): joins the row statistics, decides, then w / noise over its
- *                    chunk of the one row that the next token is drawn from
- *   k_verify_finish  (sequence): the best of the chunks
+ *                    chunk of the one row that the next token is drawn from; the last workgroup of a
+ *                    sequence to finish takes the best of its chunks (a maximum, so their order is free)
  *
- * Bound by HBM at large batches (the rows once, one row and the noise again), by three launches'
- * latency at small ones.  exp((l - m) / T) is taken as exp2((l - m) * (log2 e / T)): the one rounding
- * of the product costs 2^-24 |l - m| / T relative, below 1e-6 for every token that can matter.
+ * Bound by HBM at large batches (the rows once, one row and the noise again), by two launches' chains of
+ * dependent loads at small ones.  exp((l - m) / T) is taken as exp2((l - m) * (log2 e / T)): the one
+ * rounding of the product costs 2^-24 |l - m| / T relative, below 1e-6 for every token that can matter.
  */
 #include <hip/hip_runtime.h>
 
@@ -21,8 +21,7 @@
 namespace wsr_step {
 
 constexpr int VT = 256;                       /* threads */
-constexpr int VU = 8;                         /* 16-byte loads per thread */
-constexpr int CHUNK = VT * VU * 4;
+/* VU: 16-byte loads per thread; a chunk is VT * VU * 4 logits */
 constexpr float NEG_INF = -__builtin_inff();
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -62,6 +61,7 @@ __device__ __forceinline__ const float* row_of(const wsr_verify& p, int b, int r
 }
 
 /* A thread's VU runs of four elements of a chunk; `fill` past the row's end. */
+template <int VU>
 __device__ __forceinline__ void load_chunk(const float* row, int64_t at, int64_t n, float fill, float (&v)[VU][4]) {
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
@@ -80,23 +80,24 @@ __device__ __forceinline__ void load_chunk(const float* row, int64_t at, int64_t
 __device__ __forceinline__ void better(float& w, int& i, float w2, int i2) {
     if (w2 > w || (w2 == w && i2 < i)) w = w2, i = i2;
 }
+/* The largest w of a wave and the lowest index that has it. */
 __device__ __forceinline__ void wave_best(float& w, int& i) {
-#pragma unroll
-    for (int k = 32; k; k >>= 1) {
-        const float w2 = __shfl_xor(w, k);
-        const int i2 = __shfl_xor(i, k);
-        better(w, i, w2, i2);
-    }
+    const float top = wave_max(w);
+    i = wave_min(w == top ? i : 0x7fffffff);
+    w = top;
 }
 
-__global__ __launch_bounds__(VT) void k_verify_stats(wsr_verify p, Stat* stats, int rows, int chunks) {
+template <int VU>
+__global__ __launch_bounds__(VT) void k_verify_stats(wsr_verify p, Stat* stats, uint32_t* done, int rows, int chunks) {
+    constexpr int CHUNK = VT * VU * 4;
     __shared__ float sm[VT / WAVE], ss[VT / WAVE];
     __shared__ int si[VT / WAVE];
     const int c = blockIdx.x % chunks, r = blockIdx.x / chunks % rows, b = blockIdx.x / chunks / rows;
+    if (c == 0 && r == 0 && threadIdx.x == 0) done[b] = 0;    /* for the race's workgroups to count themselves */
     const float* row = row_of(p, b, r, count_of(p, b));
     if (!row) return;
     float v[VU][4];
-    load_chunk(row, (int64_t)c * CHUNK, p.vocab, NEG_INF, v);
+    load_chunk<VU>(row, (int64_t)c * CHUNK, p.vocab, NEG_INF, v);
     float m = NEG_INF;
     int at = 0x7fffffff;
 #pragma unroll
@@ -124,18 +125,18 @@ __global__ __launch_bounds__(VT) void k_verify_stats(wsr_verify p, Stat* stats, 
     if (threadIdx.x == 0) stats[((int64_t)b * rows + r) * chunks + c] = Stat{m, s, at, 0};
 }
 
-/* A row's statistics from its chunks, by one wave. */
-__device__ __forceinline__ Stat join_row(const Stat* st, int chunks, float t) {
-    const int lane = threadIdx.x % WAVE;
-    float m = NEG_INF;
+/* A row's statistics from its chunks, by sixteen lanes (lane j takes chunks j, j + 16, ...). */
+__device__ __forceinline__ Stat join_row(const Stat* st, int chunks, float k, int j) {
+    float m = NEG_INF, s = 0.f;
     int at = 0x7fffffff;
-    for (int c = lane; c < chunks; c += WAVE) better(m, at, st[c].m, st[c].at);
-    wave_best(m, at);
-    const float k = factor_of(t);
-    float s = 0.f;
-    for (int c = lane; c < chunks; c += WAVE)
-        if (st[c].m > NEG_INF) s += st[c].s * exp_from(st[c].m, m, k);
-    return Stat{m, wsr::wave_sum(s), at, 0};
+    for (int c = j; c < chunks; c += 16) {
+        const Stat o = st[c];
+        if (o.m > m) s = s * (m > NEG_INF ? exp_from(m, o.m, k) : 0.f) + o.s, m = o.m, at = o.at;
+        else if (o.m > NEG_INF) s += o.s * exp_from(o.m, m, k);
+    }
+    const float top = row_max(m);
+    at = row_min(m == top ? at : 0x7fffffff);
+    return Stat{top, row_sum(m > NEG_INF ? s * exp_from(m, top, k) : 0.f), at, 0};
 }
 
 /* The probability of logit l (index i) in a row. */
@@ -154,52 +155,55 @@ __device__ __forceinline__ float log_prob(float l, int i, const Stat& st, float 
 
 constexpr int MAX_ROWS = 2 * 63 + 1;
 
-__global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* stats, Best* best, Stat* last, int rows,
+template <int VU>
+__global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* stats, Best* best, uint32_t* done, int rows,
                                                     int chunks) {
+    constexpr int CHUNK = VT * VU * 4;
     __shared__ Stat all[MAX_ROWS];
     __shared__ float sw[VT / WAVE], sp[VT / WAVE];
-    __shared__ int swi[VT / WAVE], spi[VT / WAVE], verdict;
+    __shared__ int swi[VT / WAVE], spi[VT / WAVE], verdict, last;
     const int c = blockIdx.x % chunks, b = blockIdx.x / chunks, wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
     const int count = count_of(p, b), n = p.n_drafts;
     const float t = temperature_of(p, b), k = factor_of(t);
-    for (int r = wave; r < rows; r += VT / WAVE) {
+    /* what does not wait for the statistics: the noise, and (by the first wave) each draft and its logits */
+    float v[VU][4], z[VU][4], q[VU][4];
+    load_chunk<VU>((const float*)((const char*)p.noise + b * p.noise_seq_stride), (int64_t)c * CHUNK, p.vocab, 1.f, z);
+    int x = -1;
+    float u = 0.f, lt = NEG_INF, ld = NEG_INF;
+    if (wave == 0 && lane < count) {
+        x = p.tokens[(int64_t)b * n + lane];
+        u = p.uniform[(int64_t)b * n + lane];
+        if (x >= 0 && x < p.vocab) {
+            lt = row_of(p, b, lane, count)[x];
+            if (p.draft) ld = row_of(p, b, n + 1 + lane, count)[x];
+        }
+    }
+    for (int r = threadIdx.x / 16; r < rows; r += VT / 16) {
         if (!row_of(p, b, r, count)) continue;
-        const Stat st = join_row(stats + ((int64_t)b * rows + r) * chunks, chunks, t);
-        if (lane == 0) all[r] = st;
+        const Stat st = join_row(stats + ((int64_t)b * rows + r) * chunks, chunks, k, threadIdx.x % 16);
+        if (threadIdx.x % 16 == 0) all[r] = st;
     }
     __syncthreads();
     if (wave == 0) {
         /* lane i judges draft i */
         bool pass = false;
         float lp = 0.f;
-        if (lane < count) {
-            const int x = p.tokens[(int64_t)b * n + lane];
-            if (x >= 0 && x < p.vocab) {
-                const Stat& st = all[lane];
-                const float l = row_of(p, b, lane, count)[x];
-                const float px = prob(l, x, st, 1.f / st.s, k);
-                float qx = 1.f;
-                if (p.draft) {
-                    const Stat& sq = all[n + 1 + lane];
-                    qx = prob(row_of(p, b, n + 1 + lane, count)[x], x, sq, 1.f / sq.s, k);
-                }
-                pass = p.uniform[(int64_t)b * n + lane] * qx < px;
-                lp = log_prob(l, x, st, t);
-            }
+        if (x >= 0 && x < p.vocab) {
+            const Stat& st = all[lane];
+            const float px = prob(lt, x, st, 1.f / st.s, k);
+            float qx = 1.f;
+            if (p.draft) qx = prob(ld, x, all[n + 1 + lane], 1.f / all[n + 1 + lane].s, k);
+            pass = u * qx < px;
+            lp = log_prob(lt, x, st, t);
         }
-        const uint64_t failed = ~__ballot(pass);
-        const int accepted = __builtin_ctzll(failed);        /* lane 63 never passes: count <= 63 */
+        const int accepted = __builtin_ctzll(~__ballot(pass));   /* lane 63 never passes: count <= 63 */
         if (lane == 0) verdict = accepted;
         if (c == 0) {
-            for (int i = lane; i <= n; i += WAVE) {
-                if (i < accepted) p.out[(int64_t)b * (n + 1) + i] = p.tokens[(int64_t)b * n + i];
-                else if (i > accepted) p.out[(int64_t)b * (n + 1) + i] = -1;
-                if (p.logp) {
-                    if (i < accepted) p.logp[(int64_t)b * (n + 1) + i] = lp;
-                    else if (i > accepted) p.logp[(int64_t)b * (n + 1) + i] = 0.f;
-                }
+            if (lane <= n && lane != accepted) {
+                p.out[(int64_t)b * (n + 1) + lane] = lane < accepted ? x : -1;
+                if (p.logp) p.logp[(int64_t)b * (n + 1) + lane] = lane < accepted ? lp : 0.f;
             }
-            if (lane == 0) p.accepted[b] = accepted, last[b] = all[accepted];
+            if (lane == 0) p.accepted[b] = accepted;
         }
     }
     __syncthreads();
@@ -208,28 +212,25 @@ __global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* st
     const bool residual = a < count;
     const float* prow = row_of(p, b, a, count);
     const float* qrow = residual && p.draft ? row_of(p, b, n + 1 + a, count) : nullptr;
+    load_chunk<VU>(prow, (int64_t)c * CHUNK, p.vocab, NEG_INF, v);
+    if (qrow) load_chunk<VU>(qrow, (int64_t)c * CHUNK, p.vocab, NEG_INF, q);
     const Stat sq = qrow ? all[n + 1 + a] : Stat{0.f, 1.f, 0, 0};
-    const int x = residual && !p.draft ? p.tokens[(int64_t)b * n + a] : -1;
+    const int point = residual && !p.draft ? p.tokens[(int64_t)b * n + a] : -1;
     const float ip = 1.f / st.s, iq = 1.f / sq.s;
-    float v[VU][4], z[VU][4], q[VU][4];
-    load_chunk((const float*)((const char*)p.noise + b * p.noise_seq_stride), (int64_t)c * CHUNK, p.vocab, 1.f, z);
-    load_chunk(prow, (int64_t)c * CHUNK, p.vocab, NEG_INF, v);
-    if (qrow) load_chunk(qrow, (int64_t)c * CHUNK, p.vocab, NEG_INF, q);
     float bw = 0.f, bp = 0.f;
     int bwi = 0x7fffffff, bpi = 0x7fffffff;
 #pragma unroll
-    for (int u = 0; u < VU; ++u)
+    for (int e = 0; e < VU; ++e)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int i = c * CHUNK + (u * VT + (int)threadIdx.x) * 4 + j;
-            if (i >= p.vocab) continue;
-            const float pv = prob(v[u][j], i, st, ip, k);
+            const int i = c * CHUNK + (e * VT + (int)threadIdx.x) * 4 + j;
+            const float pv = prob(v[e][j], i, st, ip, k);        /* 0 past the row's end */
             float w = pv;
-            if (qrow) w = pv - prob(q[u][j], i, sq, iq, k);
-            else if (i == x) w = pv - 1.f;
-            const float rn = 1.f / z[u][j];
+            if (qrow) w = pv - prob(q[e][j], i, sq, iq, k);
+            else if (i == point) w = pv - 1.f;
+            const float rn = __builtin_amdgcn_rcpf(z[e][j]);
             if (w > 0.f && w * rn > bw) bw = w * rn, bwi = i;
-            if (pv > 0.f && pv * rn > bp) bp = pv * rn, bpi = i;
+            if (pv * rn > bp) bp = pv * rn, bpi = i;
         }
     wave_best(bw, bwi);
     wave_best(bp, bpi);
@@ -239,60 +240,65 @@ __global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* st
 #pragma unroll
         for (int w = 1; w < VT / WAVE; ++w) better(bw, bwi, sw[w], swi[w]), better(bp, bpi, sp[w], spi[w]);
         best[(int64_t)b * chunks + c] = Best{bw, bp, bwi, bpi};
+        /* releases this workgroup's best to, and acquires the others' for, whichever counts last */
+        last = __hip_atomic_fetch_add(&done[b], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)chunks - 1;
     }
-}
-
-__global__ __launch_bounds__(WAVE) void k_verify_finish(wsr_verify p, const Best* best, const Stat* last, int chunks) {
-    const int b = blockIdx.x, lane = threadIdx.x;
-    float w = 0.f, q = 0.f;
-    int wi = 0x7fffffff, qi = 0x7fffffff;
-    for (int c = lane; c < chunks; c += WAVE) {
-        const Best o = best[(int64_t)b * chunks + c];
+    __syncthreads();
+    if (!last || wave) return;
+    float w = 0.f, f = 0.f;
+    int wi = 0x7fffffff, fi = 0x7fffffff;
+    for (int i = lane; i < chunks; i += WAVE) {
+        const Best o = best[(int64_t)b * chunks + i];
         better(w, wi, o.w, o.wi);
-        better(q, qi, o.p, o.pi);
+        better(f, fi, o.p, o.pi);
     }
     wave_best(w, wi);
-    wave_best(q, qi);
+    wave_best(f, fi);
     if (lane) return;
-    const int token = w > 0.f ? wi : q > 0.f ? qi : -1;
-    const int a = p.accepted[b];
-    const int64_t at = (int64_t)b * (p.n_drafts + 1) + a;
-    p.out[at] = token;
-    if (p.logp) p.logp[at] = token < 0 ? NEG_INF : log_prob(row_of(p, b, a, a)[token], token, last[b], temperature_of(p, b));
+    const int token = w > 0.f ? wi : f > 0.f ? fi : -1;
+    p.out[(int64_t)b * (n + 1) + a] = token;
+    if (p.logp) p.logp[(int64_t)b * (n + 1) + a] = token < 0 ? NEG_INF : log_prob(prow[token], token, st, t);
 }
 
 struct VerifyPlan {
     int rows, chunks;
-    size_t best_at, last_at, bytes;
+    bool fine;
+    size_t best_at, done_at, bytes;
 };
 static VerifyPlan plan_of(const wsr_verify& p) {
     VerifyPlan v;
     v.rows = p.n_drafts + 1 + (p.draft ? p.n_drafts : 0);
-    v.chunks = (int)((p.vocab + CHUNK - 1) / CHUNK);
+    /* chunks of 8192 logits, of 2048 where the former would leave most of the chip idle in the race */
+    const int64_t wide = (p.vocab + VT * 32 - 1) / (VT * 32);
+    v.fine = p.n_seqs * wide < 256;
+    v.chunks = (int)(v.fine ? (p.vocab + VT * 8 - 1) / (VT * 8) : wide);
     const size_t pairs = (size_t)p.n_seqs * v.chunks;
     v.best_at = (pairs * v.rows * sizeof(Stat) + 255) / 256 * 256;
-    v.last_at = v.best_at + (pairs * sizeof(Best) + 255) / 256 * 256;
-    v.bytes = v.last_at + (size_t)p.n_seqs * sizeof(Stat);
+    v.done_at = v.best_at + (pairs * sizeof(Best) + 255) / 256 * 256;
+    v.bytes = v.done_at + (size_t)p.n_seqs * sizeof(uint32_t);
     return v;
 }
 
 size_t verify_workspace(const wsr_verify& p) { return plan_of(p).bytes; }
 
-hipError_t launch_verify(const wsr_verify& p, void* ws, hipStream_t s) {
-    const VerifyPlan v = plan_of(p);
-    Stat* stats = static_cast<Stat*>(ws);
-    Best* best = reinterpret_cast<Best*>(static_cast<char*>(ws) + v.best_at);
-    Stat* last = reinterpret_cast<Stat*>(static_cast<char*>(ws) + v.last_at);
+template <int VU>
+static hipError_t launch_two(const wsr_verify& p, const VerifyPlan& v, char* ws, hipStream_t s) {
+    Stat* stats = reinterpret_cast<Stat*>(ws);
+    Best* best = reinterpret_cast<Best*>(ws + v.best_at);
+    uint32_t* done = reinterpret_cast<uint32_t*>(ws + v.done_at);
     const int64_t blocks = (int64_t)p.n_seqs * v.rows * v.chunks;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k_verify_stats, dim3((unsigned)blocks), dim3(VT), 0, s, p, stats, v.rows, v.chunks);
-    hipError_t e = hipGetLastError();
+    hipLaunchKernelGGL(k_verify_stats<VU>, dim3((unsigned)blocks), dim3(VT), 0, s, p, stats, done, v.rows, v.chunks);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_verify_race, dim3((unsigned)(p.n_seqs * v.chunks)), dim3(VT), 0, s, p, stats, best, last, v.rows,
+    hipLaunchKernelGGL(k_verify_race<VU>, dim3((unsigned)(p.n_seqs * v.chunks)), dim3(VT), 0, s, p, stats, best, done, v.rows,
                        v.chunks);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(k_verify_finish, dim3((unsigned)p.n_seqs), dim3(WAVE), 0, s, p, best, last, v.chunks);
     return hipGetLastError();
+}
+
+hipError_t launch_verify(const wsr_verify& p, void* ws, hipStream_t s) {
+    const VerifyPlan v = plan_of(p);
+    return v.fine ? launch_two<2>(p, v, static_cast<char*>(ws), s) : launch_two<8>(p, v, static_cast<char*>(ws), s);
 }
 
 }  // namespace wsr_step
