@@ -16,10 +16,14 @@ typedef __attribute__((address_space(1))) f4_t g_f4;
 typedef const __attribute__((address_space(1))) u32x4 g_cu4;
 typedef __attribute__((address_space(1))) u32x4 g_u4;
 
-/* u <- (u - mean) / sqrt(var + eps) * w + b over the row's d elements (RMS: mean = 0). */
+/* Whether the weights are loaded at the start: with four pieces per thread there are no registers for them. */
+template <int NC>
+constexpr bool early() { return NC < 4; }
+
+/* u <- (u - mean) / sqrt(var + eps) * w + b over the row's d elements (RMS: mean = 0); w and b where given. */
 template <int FMT, int KIND, int WAVES, int NC>
-__device__ __forceinline__ void norm_row(float (&u)[NC][8], const void* w, const void* b, int64_t d, float eps,
-                                         float (&s0)[WAVES], float (&s1)[WAVES]) {
+__device__ __forceinline__ void norm_row(float (&u)[NC][8], const u32x4 (&w)[NC], const u32x4 (&b)[NC], const void* wp,
+                                         const void* bp, int d, float eps, float (&s0)[WAVES], float (&s1)[WAVES]) {
     const float inv_d = 1.f / (float)d;
     if constexpr (KIND == WSR_NORM_LAYER) {
         float sum = 0.f;
@@ -30,7 +34,7 @@ __device__ __forceinline__ void norm_row(float (&u)[NC][8], const void* w, const
         const float mean = block_sum<WAVES>(sum, s0) * inv_d;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
-            if ((int64_t)(threadIdx.x + c * WAVES * WAVE) * 8 < d)
+            if ((int)(threadIdx.x + c * WAVES * WAVE) * 8 < d)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) u[c][j] -= mean;
     }
@@ -42,78 +46,104 @@ __device__ __forceinline__ void norm_row(float (&u)[NC][8], const void* w, const
     const float r = 1.f / sqrtf(block_sum<WAVES>(sq, s1) * inv_d + eps);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int64_t i = threadIdx.x + c * WAVES * WAVE;
+        const int i = threadIdx.x + c * WAVES * WAVE;
         if (i * 8 >= d) continue;
         float wv[8], bv[8];
-        if (w) unpack8<FMT>(((g_cu4*)w)[i], wv);
-        if (b) unpack8<FMT>(((g_cu4*)b)[i], bv);
+        if (wp) unpack8<FMT>(early<NC>() ? w[c] : ((g_cu4*)wp)[i], wv);
+        if (bp) unpack8<FMT>(early<NC>() ? b[c] : ((g_cu4*)bp)[i], bv);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             u[c][j] *= r;
-            if (w) u[c][j] *= wv[j];
-            if (b) u[c][j] += bv[j];
+            if (wp) u[c][j] *= wv[j];
+            if (bp) u[c][j] += bv[j];
         }
     }
 }
 
-/* One workgroup per token; thread i holds elements 8 i .. 8 i + 7 of each run of 8 * threads. */
-template <int FMT, int KIND, int WAVES, int NC>
+/* One workgroup per token; thread i holds elements 8 i .. 8 i + 7 of each run of 8 * threads.  All of the row's
+   inputs are loaded at the start (with the gate and the weights loaded where they are used, 4099 x 8192 layer
+   norms took 107 us, so 101; one token of 4096 3.43 and 3.30).  STREAM: h' is stored past the caches. */
+template <int FMT, int KIND, int WAVES, int NC, bool STREAM>
 __global__ __launch_bounds__(WAVES * WAVE) void k_block_norm(wsr_block p) {
     __shared__ float red[4][WAVES];
     const int64_t t = blockIdx.x;
+    const int d = (int)p.d;
     float u[NC][8], h[NC][8];
+    u32x4 gate[NC], w0[NC], b0[NC], w1[NC], b1[NC];
     const char* yr = (const char*)p.y + t * p.y_tok_stride;
     const char* hr = (const char*)p.h + t * p.h_tok_stride;
+    const char* gr = (const char*)p.gate + t * p.gate_tok_stride;
+    const bool post = p.y && (p.flags & WSR_BLOCK_POST);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int64_t i = threadIdx.x + c * WAVES * WAVE;
-        const bool in = i * 8 < p.d;
+        const int i = threadIdx.x + c * WAVES * WAVE;
+        const bool in = i * 8 < d;
         f4_t a = {0, 0, 0, 0}, b = a, e = a, f = a;
-        if (in && p.y) a = ((g_cf4*)yr)[2 * i], b = ((g_cf4*)yr)[2 * i + 1];
-        if (in && p.h) e = ((g_cf4*)hr)[2 * i], f = ((g_cf4*)hr)[2 * i + 1];
+        gate[c] = w0[c] = b0[c] = w1[c] = b1[c] = wsr::zero4();
+        if (in) {
+            if (p.y) a = ((g_cf4*)yr)[2 * i], b = ((g_cf4*)yr)[2 * i + 1];
+            if (p.h) e = ((g_cf4*)hr)[2 * i], f = ((g_cf4*)hr)[2 * i + 1];
+            if (p.gate) gate[c] = ((g_cu4*)gr)[i];
+            if constexpr (early<NC>()) {
+                if (post && p.post_w) w0[c] = ((g_cu4*)p.post_w)[i];
+                if (post && p.post_b) b0[c] = ((g_cu4*)p.post_b)[i];
+                if (p.x && p.pre_w) w1[c] = ((g_cu4*)p.pre_w)[i];
+                if (p.x && p.pre_b) b1[c] = ((g_cu4*)p.pre_b)[i];
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) u[c][j] = a[j], u[c][4 + j] = b[j], h[c][j] = e[j], h[c][4 + j] = f[j];
     }
-    if (p.y && (p.flags & WSR_BLOCK_POST))
-        norm_row<FMT, KIND, WAVES, NC>(u, p.post_w, p.post_b, p.d, p.eps, red[0], red[1]);
-    const char* gr = (const char*)p.gate + t * p.gate_tok_stride;
+    if (post) norm_row<FMT, KIND, WAVES, NC>(u, w0, b0, p.post_w, p.post_b, d, p.eps, red[0], red[1]);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int64_t i = threadIdx.x + c * WAVES * WAVE;
-        if (i * 8 >= p.d) continue;
+        const int i = threadIdx.x + c * WAVES * WAVE;
+        if (i * 8 >= d) continue;
         if (p.gate) {
             float g[8];
-            unpack8<FMT>(((g_cu4*)gr)[i], g);
+            unpack8<FMT>(gate[c], g);
 #pragma unroll
             for (int j = 0; j < 8; ++j) u[c][j] *= g[j];
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) u[c][j] = p.h ? fmaf(p.res_scale, h[c][j], u[c][j]) : u[c][j];
         if (p.h_out) {
-            g_f4* o = (g_f4*)((char*)p.h_out + t * p.h_out_tok_stride);
-            o[2 * i] = f4_t{u[c][0], u[c][1], u[c][2], u[c][3]};
-            o[2 * i + 1] = f4_t{u[c][4], u[c][5], u[c][6], u[c][7]};
+            g_f4* o = (g_f4*)((char*)p.h_out + t * p.h_out_tok_stride) + 2 * i;
+            const f4_t a = {u[c][0], u[c][1], u[c][2], u[c][3]}, b = {u[c][4], u[c][5], u[c][6], u[c][7]};
+            if constexpr (STREAM) __builtin_nontemporal_store(a, o), __builtin_nontemporal_store(b, o + 1);
+            else o[0] = a, o[1] = b;
         }
     }
     if (!p.x) return;
-    norm_row<FMT, KIND, WAVES, NC>(u, p.pre_w, p.pre_b, p.d, p.eps, red[2], red[3]);
+    norm_row<FMT, KIND, WAVES, NC>(u, w1, b1, p.pre_w, p.pre_b, d, p.eps, red[2], red[3]);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int64_t i = threadIdx.x + c * WAVES * WAVE;
-        if (i * 8 >= p.d) continue;
+        const int i = threadIdx.x + c * WAVES * WAVE;
+        if (i * 8 >= d) continue;
         ((g_u4*)((char*)p.x + t * p.x_tok_stride))[i] =
             u32x4{pack2<FMT>(u[c][0], u[c][1]), pack2<FMT>(u[c][2], u[c][3]), pack2<FMT>(u[c][4], u[c][5]),
                   pack2<FMT>(u[c][6], u[c][7])};
     }
 }
 
+/* Few tokens: as many threads as the row has pieces, for the shortest chain.  Many tokens of 4104 to 8192
+   elements: two pieces each (4099 tokens 111.8 us with one, so 107.2; 16 tokens 4.62 and 4.73, 64 tokens 5.70 and
+   6.14).  A residual stream larger than the chip's second-level caches is gone from them before it is read
+   again, so it is stored past them (8193 x 4096 86.8 us, so 84.8; 8193 x 1160 29.4 and 26.1). */
+constexpr int64_t STREAM_FROM = 32 << 20;
 template <int FMT, int KIND>
 static void launch_kind(const wsr_block& p, hipStream_t s) {
-#define WSR_NORM(W, NC) \
-    hipLaunchKernelGGL((k_block_norm<FMT, KIND, W, NC>), dim3((unsigned)p.n_tokens), dim3(W * WAVE), 0, s, p)
+    const bool stream = p.n_tokens * p.d * 4 >= STREAM_FROM;
+#define WSR_NORM(W, NC)                                                                                                      \
+    do {                                                                                                                     \
+        const dim3 grid((unsigned)p.n_tokens), threads(W * WAVE);                                                            \
+        if (stream) hipLaunchKernelGGL((k_block_norm<FMT, KIND, W, NC, true>), grid, threads, 0, s, p);                      \
+        else hipLaunchKernelGGL((k_block_norm<FMT, KIND, W, NC, false>), grid, threads, 0, s, p);                            \
+    } while (0)
     if (p.d <= 512) WSR_NORM(1, 1);
     else if (p.d <= 2048) WSR_NORM(4, 1);
     else if (p.d <= 4096) WSR_NORM(8, 1);
+    else if (p.d <= 8192 && p.n_tokens >= 512) WSR_NORM(8, 2);
     else if (p.d <= 8192) WSR_NORM(16, 1);
     else if (p.d <= 16384) WSR_NORM(16, 2);
     else WSR_NORM(16, 4);
