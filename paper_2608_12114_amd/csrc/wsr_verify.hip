@@ -240,8 +240,10 @@ __global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* st
 #pragma unroll
         for (int w = 1; w < VT / WAVE; ++w) better(bw, bwi, sw[w], swi[w]), better(bp, bpi, sp[w], spi[w]);
         best[(int64_t)b * chunks + c] = Best{bw, bp, bwi, bpi};
-        /* releases this workgroup's best to, and acquires the others' for, whichever counts last */
-        last = __hip_atomic_fetch_add(&done[b], 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)chunks - 1;
+        /* releases this workgroup's best to whichever counts last; only that one acquires (with an acquire in all
+           of them, which empties caches each time, the race of 64 sequences took 41 us, so 33) */
+        last = __hip_atomic_fetch_add(&done[b], 1u, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)chunks - 1;
+        if (last) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     }
     __syncthreads();
     if (!last || wave) return;
