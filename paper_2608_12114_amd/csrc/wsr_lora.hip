@@ -24,6 +24,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "wsr_mma.h"
 #include "wsr_step_device.h"
@@ -388,8 +389,8 @@ __device__ __forceinline__ void make_inner(const LoraMod& d, const LoraCall& c, 
 
 /* A wave's 16 RW rows of a unit against the tile's tokens, U steps of four chunks at a time. */
 template <int FMT, int TT, int RW, int N>
-__global__ __launch_bounds__(LT) void k_lora_expand(LoraTable<N> tab, LoraCall c) {
-    constexpr int COLS = 16 * TT, ROWS = LW * 16 * RW, U = TT == 1 ? 16 / RW : 2, NTERM = terms<FMT>();
+__global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_lora_expand(LoraTable<N> tab, LoraCall c) {
+    constexpr int COLS = 16 * TT, ROWS = LW * 16 * RW, U = TT == 1 ? 4 : 2, NTERM = terms<FMT>();
     typedef Inner<FMT, COLS> I;
     __shared__ Tile<COLS> t;
     __shared__ I in;
@@ -398,6 +399,10 @@ __global__ __launch_bounds__(LT) void k_lora_expand(LoraTable<N> tab, LoraCall c
     share_of(tab.units, c.tiles, tile, u0, u1);
     if (u0 >= u1) return;
     const int used = min(TT, (c.n_tokens - tile * TILE + 15) / 16);    /* token tiles that hold tokens */
+    /* Outputs are read and written as whole 128-byte lines: the sums of two 16-row tiles change places so that one
+       access takes both tiles of eight tokens (col / 8 the tile), the next those of the other eight.  Access i: */
+    auto out_col = [&](int i) { return RW > 1 ? i % 2 * 8 + col % 8 : col; };
+    auto out_row = [&](int i) { return RW > 1 ? i / 2 * 32 + col / 8 * 16 + 4 * g : 16 * i + 4 * g; };
     int m = mod_of(tab, u0);
     for (int unit = u0; unit < u1; ++unit) {
         while (m + 1 < tab.n && tab.first[m + 1] <= unit) ++m;
@@ -413,12 +418,13 @@ __global__ __launch_bounds__(LT) void k_lora_expand(LoraTable<N> tab, LoraCall c
             }
             if (w0 == 0 && whole && d.y0) {
 #pragma unroll
-                for (int j = 0; j < TT; ++j) {
-                    const int tok = t.tok[16 * j + col];
-                    const float* src = (const float*)((const char*)d.y0 + (tok < 0 ? t.tok[0] : tok) * d.y0_stride) + i0 + 4 * g;
+                for (int j = 0; j < TT; ++j)
 #pragma unroll
-                    for (int i = 0; i < RW; ++i) y0[i][j] = *(const f4_any_t*)(src + 16 * i);
-                }
+                    for (int i = 0; i < RW; ++i) {
+                        const int tok = t.tok[16 * j + out_col(i)];
+                        const float* src = (const float*)((const char*)d.y0 + (tok < 0 ? t.tok[0] : tok) * d.y0_stride);
+                        y0[i][j] = *(const f4_any_t*)(src + i0 + out_row(i));
+                    }
             }
             if (t.chunks == 0) break;          /* no adapter reaches this window or a later one */
             if (inner != m || d.rank > WINDOW) {
@@ -434,14 +440,14 @@ __global__ __launch_bounds__(LT) void k_lora_expand(LoraTable<N> tab, LoraCall c
             int64_t row[RW];
 #pragma unroll
             for (int i = 0; i < RW; ++i) row[i] = min(i0 + 16 * i + col, d.M - 1) * d.rank * 2;
-            for (int c0 = 0; c0 < chunks; c0 += 4 * U) {
-                int adapter[U];
-                /* past the list's end the last chunk stands in, against no token */
+            /* U steps of four chunks, all loads before the products */
+            auto batch = [&](auto steps, int c0) {
+                constexpr int U = decltype(steps)::value;
+                int adapter[U], ch[U];
                 u32x4 b[U][RW];
-                int ch[U];
                 const char* p[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
+                for (int u = 0; u < U; ++u) {  /* past the list's end the last chunk stands in, against no token */
                     const int cell = c0 + 4 * u + g;
                     ch[u] = t.list[min(cell, chunks - 1)];
                     p[u] = (const char*)d.b + (ch[u] >> 8) * d.b_stride + (w0 + (ch[u] >> 4 & 15) * 8) * 2;
@@ -472,7 +478,7 @@ __global__ __launch_bounds__(LT) void k_lora_expand(LoraTable<N> tab, LoraCall c
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    if (c0 + 4 * u >= chunks) break;
+                    if (TT > 1 && c0 + 4 * u >= chunks) break;
                     const int chunk = (ch[u] >> 4 & 15) * 8;
 #pragma unroll
                     for (int j = 0; j < TT; ++j) {
@@ -506,32 +512,48 @@ __global__ __launch_bounds__(LT) void k_lora_expand(LoraTable<N> tab, LoraCall c
                         }
                     }
                 }
+            };
+            if constexpr (TT > 1) {            /* few steps at a time: the last may be half empty */
+                for (int c0 = 0; c0 < chunks; c0 += 4 * U) batch(std::integral_constant<int, U>{}, c0);
+            } else {
+                int c0 = 0;
+                for (; c0 + 4 * (U - 1) < chunks; c0 += 4 * U) batch(std::integral_constant<int, U>{}, c0);
+                if (c0 + 4 < chunks) batch(std::integral_constant<int, 2>{}, c0), c0 += 8;
+                if (c0 < chunks) batch(std::integral_constant<int, 1>{}, c0);
             }
         }
 #pragma unroll
         for (int j = 0; j < TT; ++j) {
-            const int tok = t.tok[16 * j + col];
-            const bool has = t.id[16 * j + col] >= 0;
-            if (tok < 0 || (!has && d.y0 == d.y)) continue;
-            const float undo = FMT == WSR_F16 && has ? in.undo[16 * j + col] : 1.f;
-            float* dst = (float*)((char*)d.y + tok * d.y_stride) + i0 + 4 * g;
-            if (whole) {
+            if constexpr (FMT == WSR_F16) {
+                const float undo = t.id[16 * j + col] >= 0 ? in.undo[16 * j + col] : 1.f;
 #pragma unroll
-                for (int i = 0; i < RW; ++i) {
-                    f4_t s = acc[i][j] * undo;
-                    if (d.y0) s = has ? y0[i][j] + s : y0[i][j];
-                    *(f4_any_t*)(dst + 16 * i) = s;
+                for (int i = 0; i < RW; ++i) acc[i][j] *= undo;
+            }
+            if constexpr (RW > 1) {
+#pragma unroll
+                for (int i = 0; i < RW; i += 2) {
+                    u32x4 a = __builtin_bit_cast(u32x4, acc[i][j]), b = __builtin_bit_cast(u32x4, acc[i + 1][j]);
+                    wsr::lines_to_slabs(a, b);
+                    acc[i][j] = __builtin_bit_cast(f4_t, a), acc[i + 1][j] = __builtin_bit_cast(f4_t, b);
                 }
-            } else {
-                const float* src = d.y0 ? (const float*)((const char*)d.y0 + tok * d.y0_stride) + i0 + 4 * g : nullptr;
+            }
 #pragma unroll
-                for (int i = 0; i < RW; ++i)
+            for (int i = 0; i < RW; ++i) {
+                const int cell = 16 * j + out_col(i), tok = t.tok[cell];
+                const bool has = t.id[cell] >= 0;
+                if (tok < 0 || (!has && d.y0 == d.y)) continue;
+                const int64_t at = i0 + out_row(i);
+                float* dst = (float*)((char*)d.y + tok * d.y_stride) + at;
+                f4_t s = acc[i][j];
+                if (whole) {
+                    if (d.y0) s = has ? y0[i][j] + s : y0[i][j];
+                    *(f4_any_t*)dst = s;
+                } else {
+                    const float* src = d.y0 ? (const float*)((const char*)d.y0 + tok * d.y0_stride) + at : nullptr;
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        if (i0 + 16 * i + 4 * g + k < d.M) {
-                            const float s = acc[i][j][k] * undo;
-                            dst[16 * i + k] = !src ? s : has ? src[16 * i + k] + s : src[16 * i + k];
-                        }
+                        if (at + k < d.M) dst[k] = !src ? s[k] : has ? src[k] + s[k] : src[k];
+                }
             }
         }
     }
@@ -579,11 +601,12 @@ __global__ __launch_bounds__(SORT_THREADS) void k_lora_sort(const int32_t* adapt
 
 static int tiles_of(int32_t n_tokens) { return (n_tokens + TILE - 1) / TILE; }
 
-/* The blocks of K of a shrink workgroup's span, and with them each projection's parts: spans that give every
-   workgroup the chip holds (two per CU) an equal share, of two blocks at least; for many tokens so long that a
-   token's parts, which the second launch adds up once per workgroup and projection, stay within 2 KiB. */
 static int64_t blocks_of(const wsr_lora& m) { return std::max<int64_t>(1, (m.K + BLOCK_K - 1) / BLOCK_K); }
-static int span_of(const wsr_lora* mods, int32_t n, int32_t n_tokens) {
+
+/* Blocks of K of a shrink workgroup's span at least: spans that give every workgroup the chip holds (two per CU) an
+   equal share, of two blocks or more; for many tokens so long that a token's parts, which the second launch adds
+   up once per workgroup and projection, stay within 2 KiB. */
+static int least_span(const wsr_lora* mods, int32_t n, int32_t n_tokens) {
     int64_t all = 0, least = 2;
     for (int32_t i = 0; i < n; ++i) {
         all += blocks_of(mods[i]);
@@ -604,19 +627,20 @@ static int32_t run_of(const wsr_lora* mods, int32_t n) {
     return i;
 }
 
-/* Places a run's projections: blocks, parts and partial inner vectors; the bytes of the latter. */
-static size_t place(const wsr_lora* mods, int32_t n, int32_t n_tokens, LoraMod* out, char* ws) {
-    const int span = span_of(mods, n, n_tokens);
+/* Places a run's projections: blocks, parts and partial inner vectors; the bytes of the latter, enough for spans of
+   `least` blocks or more. */
+static size_t place(const wsr_lora* mods, int32_t n, int32_t n_tokens, int least, int span, LoraMod* out, char* ws) {
     int64_t block = 0;
     size_t bytes = 0;
     for (int32_t i = 0; i < n; ++i) {
         const wsr_lora& m = mods[i];
-        const int64_t last = block + blocks_of(m) - 1;
-        const int pitch = (m.rank + 7) / 8 * 8, parts = (int)(last / span - block / span + 1);
+        const int64_t count = blocks_of(m), last = block + count - 1;
+        const int pitch = (m.rank + 7) / 8 * 8;
         if (out)
             out[i] = LoraMod{m.a, m.b, m.x, m.y0, m.y, reinterpret_cast<float*>(ws + bytes), m.a_stride, m.b_stride,
-                             m.x_tok_stride, m.y0_tok_stride, m.y_tok_stride, m.M, m.K, m.rank, pitch, parts, (int32_t)block};
-        bytes += up256((size_t)parts * n_tokens * pitch * 4);
+                             m.x_tok_stride, m.y0_tok_stride, m.y_tok_stride, m.M, m.K, m.rank, pitch,
+                             (int)(last / span - block / span + 1), (int32_t)block};
+        bytes += up256((size_t)((count + least - 2) / least + 1) * n_tokens * pitch * 4);
         block = last + 1;
     }
     return bytes;
@@ -626,7 +650,8 @@ size_t lora_workspace(const wsr_lora* mods, int32_t n, int32_t n_tokens) {
     size_t most = 256;                         /* the runs follow one another and share it */
     for (int32_t i = 0; i < n;) {
         const int32_t k = run_of(mods + i, n - i);
-        most = std::max(most, place(mods + i, k, n_tokens, nullptr, nullptr));
+        const int least = least_span(mods + i, k, n_tokens);
+        most = std::max(most, place(mods + i, k, n_tokens, least, least, nullptr, nullptr));
         i += k;
     }
     return order_bytes(n_tokens) + most;
@@ -654,43 +679,31 @@ static hipError_t launch_expand(LoraTable<N>& tab, const LoraCall& c, hipStream_
 }
 
 template <int FMT, int TT, int N>
-static hipError_t launch_pair(LoraTable<N>& tab, LoraCall c, hipStream_t s) {
-    int64_t blocks = 0, rows = 0, rank = 0;
-    for (int i = 0; i < tab.n; ++i) {
-        blocks = tab.mod[i].block0 + std::max<int64_t>(1, (tab.mod[i].K + BLOCK_K - 1) / BLOCK_K);
-        tab.first[i] = tab.mod[i].block0;
-        rows += tab.mod[i].M;
-        rank = std::max<int64_t>(rank, tab.mod[i].rank);
-    }
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    tab.units = (int32_t)blocks;
-    /* chunks that a tile can have: rounds of RT 16-row tiles, two chunks each, taken by as many workgroups as
-       fill the chip.  One tile for a single adapter of 16 ranks (7.4 us with four, so 6.0) */
-    const int64_t chunks = std::min<int64_t>(std::min(16 * TT, c.n_tokens), std::max(1, c.n_adapters)) *
-                           ((std::min<int64_t>(rank, WINDOW) + 7) / 8);
-    const bool one = TT == 1 && chunks <= 2;
-    const int64_t most = one ? 1 : (chunks + 7) / 8;
-    const int64_t spans = (blocks + c.span - 1) / c.span;
-    c.slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, SHRINK_HELD / (spans * c.tiles)));
+static hipError_t launch_pair(LoraTable<N>& tab, const LoraCall& c, bool one, hipStream_t s) {
+    int64_t rows = 0;
+    for (int i = 0; i < tab.n; ++i) tab.first[i] = tab.mod[i].block0, rows += tab.mod[i].M;
+    const int64_t blocks = (int64_t)tab.units, spans = (blocks + c.span - 1) / c.span;
     if (spans * c.tiles * c.slots > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(spans * c.tiles * c.slots));
     if (one) hipLaunchKernelGGL((k_lora_shrink<FMT, 1, 1, N>), grid, dim3(LT), 0, s, tab, c);
     else hipLaunchKernelGGL((k_lora_shrink<FMT, TT, 4, N>), grid, dim3(LT), 0, s, tab, c);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    /* few rows: 64 of them per workgroup instead of 256, so that they spread over the chip */
-    if (TT == 1 && rows < 256 * 512) return launch_expand<FMT, 1, 1, N>(tab, c, s);
+    /* units of 64 rows instead of 256 where the latter would be fewer than places on the chip */
+    if constexpr (TT == 1)
+        if (rows / 256 < EXPAND_HELD) return launch_expand<FMT, 1, 1, N>(tab, c, s);
     return launch_expand<FMT, TT, 4, N>(tab, c, s);
 }
 
 template <int N>
-static hipError_t launch_table(const LoraMod* mods, int n, int fmt, const LoraCall& c, hipStream_t s) {
+static hipError_t launch_table(const LoraMod* mods, int n, int fmt, int64_t blocks, const LoraCall& c, bool one, hipStream_t s) {
     LoraTable<N> tab;
     tab.n = n;
+    tab.units = (int32_t)blocks;
     std::copy(mods, mods + n, tab.mod);
-    const bool one = c.n_tokens <= 16;
-    if (fmt == WSR_F16) return one ? launch_pair<WSR_F16, 1, N>(tab, c, s) : launch_pair<WSR_F16, 4, N>(tab, c, s);
-    return one ? launch_pair<WSR_BF16, 1, N>(tab, c, s) : launch_pair<WSR_BF16, 4, N>(tab, c, s);
+    const bool few = c.n_tokens <= 16;
+    if (fmt == WSR_F16) return few ? launch_pair<WSR_F16, 1, N>(tab, c, one, s) : launch_pair<WSR_F16, 4, N>(tab, c, one, s);
+    return few ? launch_pair<WSR_BF16, 1, N>(tab, c, one, s) : launch_pair<WSR_BF16, 4, N>(tab, c, one, s);
 }
 
 hipError_t launch_lora(const wsr_lora* mods, int32_t n, int32_t n_tokens, const int32_t* adapter_of, int32_t n_adapters,
@@ -711,9 +724,27 @@ hipError_t launch_lora(const wsr_lora* mods, int32_t n, int32_t n_tokens, const 
     LoraMod run[TABLE_MAX];
     for (int32_t i = 0; i < n;) {
         const int32_t k = run_of(mods + i, n - i);
-        place(mods + i, k, n_tokens, run, at);
-        c.span = span_of(mods + i, k, n_tokens);
-        const hipError_t e = k <= 8 ? launch_table<8>(run, k, mods[i].fmt, c, s) : launch_table<TABLE_MAX>(run, k, mods[i].fmt, c, s);
+        int64_t blocks = 0;
+        int rank = 0;
+        for (int32_t j = i; j < i + k; ++j) blocks += blocks_of(mods[j]), rank = std::max(rank, mods[j].rank);
+        if (blocks > INT32_MAX) return hipErrorInvalidValue;
+        /* chunks that a tile can have, and rounds of four 16-row tiles, two chunks each; one such tile is
+           enough for a single adapter of 16 ranks (7.4 us with four, so 6.0) */
+        const int64_t chunks = (int64_t)std::min(std::min(n_tokens, TILE), std::max(1, n_adapters)) * ((std::min(rank, WINDOW) + 7) / 8);
+        const bool one = n_tokens <= 16 && chunks <= 2;
+        const int64_t rounds = one ? 1 : (chunks + 7) / 8;
+        /* a round's loads and sums pay from about eight blocks on: where the chip's share is less, several
+           workgroups take a longer span and its rounds in turn (`slots`), and where it is more than the call has,
+           the rounds are spread over what is left */
+        const int least = least_span(mods + i, k, n_tokens);
+        c.slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, 8 / least));
+        const int64_t held = std::max<int64_t>(1, SHRINK_HELD / c.tiles);
+        c.span = (int32_t)std::max<int64_t>(least, std::min<int64_t>(8, (blocks * c.slots + held - 1) / held));
+        const int64_t spans = (blocks + c.span - 1) / c.span;
+        c.slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, held / spans));
+        place(mods + i, k, n_tokens, least, c.span, run, at);
+        const hipError_t e = k <= 8 ? launch_table<8>(run, k, mods[i].fmt, blocks, c, one, s)
+                                    : launch_table<TABLE_MAX>(run, k, mods[i].fmt, blocks, c, one, s);
         if (e != hipSuccess) return e;
         i += k;
     }
