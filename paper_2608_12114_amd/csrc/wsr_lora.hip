@@ -64,6 +64,7 @@ struct LoraCall {
     const float* scales;
     int32_t n_tokens, n_adapters, tiles;
     int32_t span, slots;                       /* blocks of a shrink workgroup; workgroups that share its rows */
+    bool stream;                               /* outputs go past the caches */
 };
 
 /* The projection that unit b belongs to: the last whose first unit is <= b. */
@@ -387,8 +388,9 @@ __device__ __forceinline__ void make_inner(const LoraMod& d, const LoraCall& c, 
     __syncthreads();
 }
 
-/* A wave's 16 RW rows of a unit against the tile's tokens, U steps of four chunks at a time. */
-template <int FMT, int TT, int RW, int N>
+/* A wave's 16 RW rows of a unit against the tile's tokens, U steps of four chunks at a time.  STREAM: outputs are
+   stored past the caches. */
+template <int FMT, int TT, int RW, bool STREAM, int N>
 __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_lora_expand(LoraTable<N> tab, LoraCall c) {
     constexpr int COLS = 16 * TT, ROWS = LW * 16 * RW, U = TT == 1 ? 4 : 2, NTERM = terms<FMT>();
     typedef Inner<FMT, COLS> I;
@@ -547,7 +549,8 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
                 f4_t s = acc[i][j];
                 if (whole) {
                     if (d.y0) s = has ? y0[i][j] + s : y0[i][j];
-                    *(f4_any_t*)dst = s;
+                    if constexpr (STREAM) __builtin_nontemporal_store(s, (f4_any_t*)dst);
+                    else *(f4_any_t*)dst = s;
                 } else {
                     const float* src = d.y0 ? (const float*)((const char*)d.y0 + tok * d.y0_stride) + at : nullptr;
 #pragma unroll
@@ -663,7 +666,7 @@ static unsigned grid_of(int64_t units, int64_t tiles, int64_t held) {
     return (unsigned)(tiles * std::max<int64_t>(1, std::min(units, held / tiles)));
 }
 
-template <int FMT, int TT, int RW, int N>
+template <int FMT, int TT, int RW, bool STREAM, int N>
 static hipError_t launch_expand(LoraTable<N>& tab, const LoraCall& c, hipStream_t s) {
     constexpr int ROWS = LW * 16 * RW;
     int64_t units = 0;
@@ -674,7 +677,7 @@ static hipError_t launch_expand(LoraTable<N>& tab, const LoraCall& c, hipStream_
     }
     if (units == 0) return hipSuccess;
     tab.units = (int32_t)units;
-    hipLaunchKernelGGL((k_lora_expand<FMT, TT, RW, N>), dim3(grid_of(units, c.tiles, EXPAND_HELD)), dim3(LT), 0, s, tab, c);
+    hipLaunchKernelGGL((k_lora_expand<FMT, TT, RW, STREAM, N>), dim3(grid_of(units, c.tiles, EXPAND_HELD)), dim3(LT), 0, s, tab, c);
     return hipGetLastError();
 }
 
@@ -691,8 +694,10 @@ static hipError_t launch_pair(LoraTable<N>& tab, const LoraCall& c, bool one, hi
     if (e != hipSuccess) return e;
     /* units of 64 rows instead of 256 where the latter would be fewer than places on the chip */
     if constexpr (TT == 1)
-        if (rows / 256 < EXPAND_HELD) return launch_expand<FMT, 1, 1, N>(tab, c, s);
-    return launch_expand<FMT, TT, 4, N>(tab, c, s);
+        if (rows / 256 < EXPAND_HELD) return launch_expand<FMT, 1, 1, false, N>(tab, c, s);
+    if constexpr (TT > 1)
+        if (c.stream) return launch_expand<FMT, TT, 4, true, N>(tab, c, s);
+    return launch_expand<FMT, TT, 4, false, N>(tab, c, s);
 }
 
 template <int N>
@@ -738,6 +743,12 @@ hipError_t launch_lora(const wsr_lora* mods, int32_t n, int32_t n_tokens, const 
            the rounds are spread over what is left */
         const int least = least_span(mods + i, k, n_tokens);
         c.slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, 8 / least));
+        /* outputs larger than the chip's second-level caches are gone from them before they are read again (779 tokens
+           over six layers of four projections 283 us, past the caches 265; 49 tokens over four layers of the 8B
+           model 126 and 121) */
+        int64_t rows = 0;
+        for (int32_t j = i; j < i + k; ++j) rows += mods[j].M;
+        c.stream = rows * n_tokens * 4 >= 32 << 20;
         const int64_t held = std::max<int64_t>(1, SHRINK_HELD / c.tiles);
         c.span = (int32_t)std::max<int64_t>(least, std::min<int64_t>(8, (blocks * c.slots + held - 1) / held));
         const int64_t spans = (blocks + c.span - 1) / c.span;
