@@ -310,6 +310,63 @@ struct Attend {
         __syncthreads();
     }
 
+    /* The products take masked keys with a probability of zero, and zero times an infinity or NaN among their values
+       would reach rows that do not see them.  Such a row is found by its output (after join()) and summed up again,
+       key by key over those it sees, against the maximum it has: nothing is paid for it in the loop (replacing such
+       values in LDS there cost 3 to 7 % of every call). */
+    __device__ __forceinline__ bool broken() const {
+        float z = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) z = fmaf(o[i][j], 0.f, z);
+        z = wsr::xchg_add<0>(z);
+        return z != z;
+    }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    }
+    /* Adds keys from .. to - 1, those before lim for this lane's row. */
+    __device__ __forceinline__ void again(const char* kb, const char* vb, int64_t stride, int from, int to, int lim, float c, int lane) {
+        const int h = lane / 32;
+        const float base = m == A_NEG_INF ? 0.f : m * c;
+#pragma unroll 1
+        for (int key = from; key < to; ++key) {
+            const char *kr = kb + key * stride, *vr = vb + key * stride;
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const u32x4 w = ((const u32x4*)kr)[2 * k + h];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float a, b, x, y;
+                    unpack2<FMT>(w[j], a, b);
+                    unpack2<FMT>(q[k][j], x, y);
+                    s = fmaf(a, x, fmaf(b, y, s));
+                }
+            }
+            s = wsr::xchg_add<0>(s);
+            const bool see = key < lim;
+            const float prob = see ? __builtin_amdgcn_exp2f(fmaf(s, c, -base)) : 0.f;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const u32x2 w = *(const u32x2*)(vr + (32 * i + 8 * j + 4 * h) * 2);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float a, b;
+                        unpack2<FMT>(see ? w[e] : 0u, a, b);
+                        o[i][4 * j + 2 * e] = fmaf(prob, a, o[i][4 * j + 2 * e]);
+                        o[i][4 * j + 2 * e + 1] = fmaf(prob, b, o[i][4 * j + 2 * e + 1]);
+                    }
+                }
+        }
+    }
+
     /* Adds up the groups' results in LDS; the first group's waves hold the row's maximum, sum (both halves)
        and output afterwards. */
     __device__ __forceinline__ void join(u32x4* lds, float c, int wave, int lane) {
@@ -422,7 +479,19 @@ void k_attn(wsr_attn p, AttnPlan pl) {
                s ? p.kv_tok_stride : p.prefix_tok_stride, b, e, s ? past + at_row : k1, low, high, c, (l_char*)lds, wave, lane);
     }
     a.join(lds, c, wave, lane);
-    if (wave >= RW || !valid) return;
+    if (wave >= RW) return;
+    if (!prefix && __ballot(a.broken())) {
+        const bool mine = a.broken();
+        if (mine) a.clear();
+#pragma unroll 1
+        for (int s = WHOLE ? 0 : 1; s < 2; ++s) {
+            const int64_t at = s ? seq * p.kv_seq_stride + head * p.kv_head_stride : head * p.prefix_head_stride;
+            const int b = WHOLE && s ? max(k0 - shared, 0) : k0, e = !s ? min(k1, shared) : WHOLE ? k1 - shared : min(k1, seen);
+            a.again((const char*)(s ? p.k : p.k_prefix) + at, (const char*)(s ? p.v : p.v_prefix) + at,
+                    s ? p.kv_tok_stride : p.prefix_tok_stride, b, e, !mine ? b : s ? past + at_row : e, c, lane);
+        }
+    }
+    if (!valid) return;
     const int h = lane / 32;
     if (WHOLE && parts == 1) {
         const float inv = a.l > 0.f ? 1.f / a.l : a.l == 0.f ? 0.f : a.l;

@@ -171,3 +171,24 @@ def test_steady_bits_other_stream_and_graph():
         got = c.out.clone()
         c.run()
         assert torch.equal(c.out, got)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("counts,lens,P,H,N", [([5, 1, 3], [40, 7, 3], 70, 8, 2), ([2] * 10, [9] * 10, 64, 16, 4),
+                                               ([130, 200], [130, 260], 100, 64, 32)])
+def test_broken_values_reach_the_queries_that_see_them_only(counts, lens, P, H, N, dt):
+    """Infinities and NaN in the keys and values of a sequence's later tokens leave its earlier queries alone."""
+    c = Case(counts, lens, P, H, N, 128, dt, seed=12)
+    whole = torch.ones(len(c.q), dtype=torch.bool, device="cuda")
+    for b, (n, own) in enumerate(zip(counts, lens)):
+        if n < 2:
+            continue
+        c.v[b, own - 1, :, 3], c.v[b, own - 1, :, 77], c.k[b, own - 1, 0, 9] = NAN, float("inf"), NAN
+        whole[c.starts[b + 1] - 1] = False
+    c.run()
+    out, lse, mag = su.attn64(c.q, c.kp, c.vp, c.k, c.v, c.starts, c.lens, c.scale)
+    u = su.U16[dt]
+    err = (c.out.double() - out).abs()
+    assert (err <= (u + 1e-4) * mag + u * out.abs() + 64 * 2.0 ** -25 * (1 + mag.amax(-1, keepdim=True)))[whole].all()
+    assert ((c.lse.double() - lse).abs() <= 2e-5)[whole].all()
+    assert torch.isnan(c.out[~whole][:, :, 3]).all() and not torch.isfinite(c.out[~whole][:, :, 77]).any()
