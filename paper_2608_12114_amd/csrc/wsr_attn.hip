@@ -37,7 +37,8 @@ constexpr float A_LOG2E = 1.4426950408889634f;
 struct AttnPlan {
     int32_t prefix_tiles, prefix_parts;    /* row tiles and key parts of the prefix (split form) */
     int32_t own_tiles, own_parts;          /* most row tiles over all sequences, most key parts of one */
-    int32_t prefix_part, own_part;         /* keys of a part */
+    int32_t own_block;                     /* keys that a workgroup takes at a time */
+    int32_t prefix_part;                   /* keys of a part of the prefix */
     int32_t most_parts;                    /* parts of a unit of the whole form's last round, at most */
     float* part;                           /* [(prefix_parts + own_parts)][n_tokens][n_heads][head_dim + 4], or
                                               whole: [HELD][128][head_dim + 4] */
@@ -101,6 +102,13 @@ __device__ __forceinline__ int count_tiles(const wsr_attn& p, int G, int rows) {
 #pragma unroll
     for (int k = 32; k; k >>= 1) n += __shfl_xor(n, k);
     return __builtin_amdgcn_readfirstlane(n);
+}
+
+/* Keys of a part of a sequence's `own` keys (split form): of at most `parts` equal ones, whole blocks, LEAST or more
+   where joining one costs less than the keys.  Taken from the length and not from the room that the cache has. */
+constexpr int LEAST = 256;
+__device__ __forceinline__ int own_part(int own, int parts, int block) {
+    return (max(LEAST, (own - 1) / max(parts, 1) + 1) + block - 1) / block * block;
 }
 
 /* The units (row tile, key head) of the whole form: the first `full` go to a workgroup each, the other `rest` to
@@ -409,7 +417,7 @@ __global__ __launch_bounds__(AT) __attribute__((amdgpu_waves_per_eu(RW == 1 ? 1 
 void k_attn(wsr_attn p, AttnPlan pl) {
     typedef Attend<FMT, D, RW> A;
     __shared__ u32x4 lds[A::LDS];
-    constexpr int ROWS = 32 * RW;
+    constexpr int ROWS = 32 * RW, BLOCK = A::KT * A::KW;
     const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), rwave = wave % RW, col = lane % 32;
     const int G = p.n_heads / p.n_kv_heads;
     int item = blockIdx.x, part = 0, parts = 1;
@@ -445,7 +453,7 @@ void k_attn(wsr_attn p, AttnPlan pl) {
     const int seen = max(0, past + min(row0 + ROWS - 1, rows - 1) / G);    /* own keys that a row of the workgroup sees */
     int k0 = 0, k1 = 0;
     if (!WHOLE) {
-        const int keys = prefix ? pl.prefix_part : pl.own_part, all = prefix ? shared : own;
+        const int keys = prefix ? pl.prefix_part : own_part(own, pl.own_parts, BLOCK), all = prefix ? shared : own;
         if ((int64_t)part * keys >= all) return;
         k0 = part * keys;
         k1 = all - k0 > keys ? k0 + keys : all;
@@ -480,11 +488,11 @@ void k_attn(wsr_attn p, AttnPlan pl) {
     }
     a.join(lds, c, wave, lane);
     if (wave >= RW) return;
-    if (!prefix && __ballot(a.broken())) {
+    if (__ballot(a.broken()) && (!prefix || (k1 - k0) % A::KT)) {
         const bool mine = a.broken();
         if (mine) a.clear();
 #pragma unroll 1
-        for (int s = WHOLE ? 0 : 1; s < 2; ++s) {
+        for (int s = WHOLE ? 0 : !prefix; s <= (WHOLE ? 1 : !prefix); ++s) {
             const int64_t at = s ? seq * p.kv_seq_stride + head * p.kv_head_stride : head * p.prefix_head_stride;
             const int b = WHOLE && s ? max(k0 - shared, 0) : k0, e = !s ? min(k1, shared) : WHOLE ? k1 - shared : min(k1, seen);
             a.again((const char*)(s ? p.k : p.k_prefix) + at, (const char*)(s ? p.v : p.v_prefix) + at,
@@ -559,7 +567,7 @@ __global__ __launch_bounds__(AT) void k_attn_join(wsr_attn p, AttnPlan pl) {
     if (seq >= 0 && tok < start_of(p, seq + 1)) {
         /* own keys that the token sees */
         const int seen = len_of(p, seq) - (start_of(p, seq + 1) - tok) + 1;
-        if (seen > 0) own = (seen - 1) / pl.own_part + 1;
+        if (seen > 0) own = (seen - 1) / own_part(len_of(p, seq), pl.own_parts, pl.own_block) + 1;
     }
     join_row<FMT, D>(p, pl.part + row * (D + 4), (int64_t)p.n_tokens * p.n_heads * (D + 4), pl.prefix_parts + own, tok, qh, lane);
 }
@@ -585,7 +593,6 @@ __global__ __launch_bounds__(AT) void k_attn_join_units(wsr_attn p, AttnPlan pl)
 
 /* ---- host ------------------------------------------------------------------------------------------ */
 
-constexpr int LEAST = 256;                     /* keys of a part */
 static int row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 
 static AttnPlan attn_plan(const wsr_attn& p) {
@@ -601,14 +608,16 @@ static AttnPlan attn_plan(const wsr_attn& p) {
     const int64_t tiles = (rows + 32 * rw - 1) / (32 * rw), per = tiles * p.n_kv_heads;
     pl.prefix_tiles = (int32_t)tiles;
     const int64_t block = rw == 4 ? 64 : 32 * (4 / rw), held = rw == 1 ? HELD / 2 : HELD;
-    auto parts = [&](int64_t keys, int64_t units, int64_t least, int32_t& part) {
+    auto parts = [&](int64_t keys, int64_t units, int32_t& part) {
         if (keys <= 0) return (int32_t)0;
         const int64_t want = std::max<int64_t>(1, held / std::max<int64_t>(1, units));
-        part = (int32_t)std::min<int64_t>((std::max(least, (keys + want - 1) / want) + block - 1) / block * block, 1 << 30);
+        part = (int32_t)std::min<int64_t>((std::max<int64_t>(LEAST, (keys + want - 1) / want) + block - 1) / block * block, 1 << 30);
         return (int32_t)((keys + part - 1) / part);
     };
-    pl.prefix_parts = parts(p.prefix_len, per, LEAST, pl.prefix_part);
-    pl.own_parts = parts(p.max_len, (int64_t)pl.own_tiles * p.n_kv_heads, LEAST, pl.own_part);
+    int32_t longest;
+    pl.prefix_parts = parts(p.prefix_len, per, pl.prefix_part);
+    pl.own_parts = parts(p.max_len, (int64_t)pl.own_tiles * p.n_kv_heads, longest);
+    pl.own_block = (int32_t)block;
     return pl;
 }
 

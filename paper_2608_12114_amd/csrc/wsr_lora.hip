@@ -13,7 +13,9 @@
  *                   row's adapter.
  *   k_lora_expand   (projection, tile, rows): four chunks side by side are the 32 terms of one
  *                   v_mfma_f32_16x16x32; a token's inner vector enters for its own adapter's chunks and as
- *                   zeros for the others.  The inner vectors are fp32 (24 bits): they enter as the sum of
+ *                   zeros for the others; tokens that were put in order have each adapter's chunks begin a product
+ *                   of their own, so that a token's sums do not depend on the tile that the order, which is free
+ *                   inside an adapter, put it in.  The inner vectors are fp32 (24 bits): they enter as the sum of
  *                   three bf16 terms (24 bits) or of two f16 terms (22 bits, each token's vector scaled by a
  *                   power of two so that its largest entry is near 2^10), products with B exact, sums fp32.
  *                   Rounding them to one 16-bit term would leave errors of 2^-9 in the fp32 outputs.
@@ -80,7 +82,8 @@ __device__ __forceinline__ int mod_of(const LoraTable<N>& tab, int b) {
     return __builtin_amdgcn_readfirstlane(m) - 1;
 }
 
-/* A tile in LDS.  A chunk of its list: adapter << 8 | (eighth of the window) << 4 | ranks it holds (1 to 8). */
+/* A tile in LDS.  A chunk of its list: adapter << 8 | (eighth of the window) << 4 | ranks it holds (1 to 8, 0 in a
+   stand-in). */
 template <int COLS>
 struct Tile {
     int32_t list[COLS * (WINDOW / 8)];
@@ -89,8 +92,9 @@ struct Tile {
     int32_t chunks, mixed, partial;            /* mixed: tokens of more than one adapter; partial: a chunk under 8 ranks */
 };
 
-/* The tile's tokens and the chunks of ranks w0 .. w0 + WINDOW - 1, by the first wave. */
-template <int COLS>
+/* The tile's tokens and the chunks of ranks w0 .. w0 + WINDOW - 1, by the first wave.  FOURS: each adapter's chunks
+   are filled up to a multiple of four with stand-ins of its last. */
+template <bool FOURS, int COLS>
 __device__ __forceinline__ void make_tile(const LoraCall& c, int tile, int rank, int w0, Tile<COLS>& t) {
     if (threadIdx.x < WAVE) {
         const int lane = threadIdx.x, at = tile * TILE + lane;
@@ -111,14 +115,15 @@ __device__ __forceinline__ void make_tile(const LoraCall& c, int tile, int rank,
             for (int j = 0; j < n; ++j)
                 if (j < lane && __builtin_amdgcn_readlane(id, j) == id) first = false;
         }
-        const int mine = first ? (min(max(r - w0, 0), WINDOW) + 7) / 8 : 0;
+        const int real = first ? (min(max(r - w0, 0), WINDOW) + 7) / 8 : 0, mine = FOURS && c.order ? (real + 3) / 4 * 4 : real;
         int sum = mine;
 #pragma unroll
         for (int k = 1; k < WAVE; k <<= 1) {
             const int o = __shfl_up(sum, k);
             if (lane >= k) sum += o;
         }
-        for (int k = 0; k < mine; ++k) t.list[sum - mine + k] = id << 8 | k << 4 | min(8, r - w0 - 8 * k);
+        for (int k = 0; k < mine; ++k)
+            t.list[sum - mine + k] = id << 8 | min(k, real - 1) << 4 | (k < real ? min(8, r - w0 - 8 * k) : 0);
         const int all = __shfl(sum, WAVE - 1);
         if (lane < COLS) {
             t.tok[lane] = tok, t.id[lane] = id, t.rank[lane] = r;
@@ -171,7 +176,7 @@ __global__ __launch_bounds__(LT) void k_lora_shrink(LoraTable<N> tab, LoraCall c
         for (int w0 = 0; w0 < d.rank; w0 += WINDOW) {
             if (made != d.rank || d.rank > WINDOW) {
                 __syncthreads();
-                make_tile<COLS>(c, tile, d.rank, w0, t);
+                make_tile<false, COLS>(c, tile, d.rank, w0, t);
                 made = d.rank;
             }
             /* a load takes 128 bytes of each of eight rows (eight tokens): lane (g, col) those at 16 (g + 4 (col / 8)) */
@@ -322,6 +327,15 @@ __device__ __forceinline__ uint32_t not_finite(u32x4 w) {
     return (((w.x & E) + ONE) | ((w.y & E) + ONE) | ((w.z & E) + ONE) | ((w.w & E) + ONE)) & 0x80008000u;
 }
 
+/* The values with infinities and NaN as zeros. */
+template <int FMT>
+__device__ __forceinline__ u32x4 finite_only(u32x4 w) {
+    constexpr uint32_t E = FMT == WSR_BF16 ? 0x7f80u : 0x7c00u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] &= ((w[i] & E) == E ? 0u : 0xffffu) | ((w[i] >> 16 & E) == E ? 0u : 0xffff0000u);
+    return w;
+}
+
 template <int FMT>
 constexpr int terms() { return FMT == WSR_BF16 ? 3 : 2; }
 
@@ -415,7 +429,7 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
         for (int w0 = 0; w0 < d.rank; w0 += WINDOW) {
             if (made != d.rank || d.rank > WINDOW) {
                 __syncthreads();
-                make_tile<COLS>(c, tile, d.rank, w0, t);
+                make_tile<true, COLS>(c, tile, d.rank, w0, t);
                 made = d.rank;
             }
             if (w0 == 0 && whole && d.y0) {
@@ -437,8 +451,11 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
             int id[TT];
 #pragma unroll
             for (int j = 0; j < TT; ++j) id[j] = t.id[16 * j + col];
-            const bool partial = __builtin_amdgcn_readfirstlane(t.partial), mixed = __builtin_amdgcn_readfirstlane(t.mixed);
+            const bool partial = __builtin_amdgcn_readfirstlane(t.partial);
             const int chunks = __builtin_amdgcn_readfirstlane(t.chunks);
+            /* zero times an infinity or NaN of one adapter's weights would reach the tokens of the others, and in a
+               stand-in make NaN of an infinity */
+            const bool watch = c.order || __builtin_amdgcn_readfirstlane(t.mixed) || chunks % 4;
             int64_t row[RW];
 #pragma unroll
             for (int i = 0; i < RW; ++i) row[i] = min(i0 + 16 * i + col, d.M - 1) * d.rank * 2;
@@ -453,7 +470,7 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
                     const int cell = c0 + 4 * u + g;
                     ch[u] = t.list[min(cell, chunks - 1)];
                     p[u] = (const char*)d.b + (ch[u] >> 8) * d.b_stride + (w0 + (ch[u] >> 4 & 15) * 8) * 2;
-                    adapter[u] = cell < chunks ? ch[u] >> 8 : -2;
+                    adapter[u] = cell < chunks && ch[u] & 15 ? ch[u] >> 8 : -2;
                 }
                 if (partial) {
 #pragma unroll
@@ -467,16 +484,16 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
                         for (int i = 0; i < RW; ++i) b[u][i] = load_weights<TT == 1>(p[u] + row[i]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                /* zero times an infinity or NaN of one adapter's weights would reach the tokens of the others:
-                   such chunks go one by one, their sums taken over by their own tokens only */
-                bool apart = false;
-                if (mixed) {
-                    uint32_t bad = 0;
+                /* steps with infinities or NaN go chunk by chunk, a chunk's sums taken over by its own tokens only */
+                uint32_t apart = 0;
+                if (watch) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
+                    for (int u = 0; u < U; ++u) {
+                        uint32_t bad = 0;
 #pragma unroll
                         for (int i = 0; i < RW; ++i) bad |= not_finite<FMT>(b[u][i]);
-                    apart = __ballot(bad != 0) != 0;
+                        apart |= __ballot(bad != 0) ? 1u << u : 0u;
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -493,20 +510,25 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
                             v[k] = *(const u32x4*)(in.v + (16 * j + col) * I::PITCH + k * WINDOW + chunk);
                             if (!own) v[k] = wsr::zero4();
                         }
-                        if (!apart) {
+                        if (!(apart >> u & 1)) {
 #pragma unroll
                             for (int k = 0; k < NTERM; ++k)
 #pragma unroll
                                 for (int i = 0; i < RW; ++i) acc[i][j] = mma_16x16x32<FMT>(b[u][i], v[k], acc[i][j]);
                         } else {
+#pragma unroll 1
                             for (int o = 0; o < 4; ++o) {
                                 const bool mine = id[j] >= 0 && id[j] == __shfl(adapter[u], 16 * o);
 #pragma unroll
                                 for (int i = 0; i < RW; ++i) {
                                     f4_t s = acc[i][j];
+                                    u32x4 w = g == o ? b[u][i] : wsr::zero4();
+                                    asm volatile("" : "+v"(w));          /* or the next line's registers are held all along */
 #pragma unroll
-                                    for (int k = 0; k < NTERM; ++k)
-                                        s = mma_16x16x32<FMT>(g == o ? b[u][i] : wsr::zero4(), g == o ? v[k] : wsr::zero4(), s);
+                                    for (int k = 0; k < NTERM; ++k) {
+                                        s = mma_16x16x32<FMT>(w, v[k], s);
+                                        if (k == 0) w = finite_only<FMT>(w);   /* later terms may differ in sign */
+                                    }
 #pragma unroll
                                     for (int e = 0; e < 4; ++e) acc[i][j][e] = mine ? s[e] : acc[i][j][e];
                                 }
@@ -563,7 +585,8 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
 }
 
 /* Tokens in the order of their adapters, those without one last.  The order inside an adapter follows from
-   the atomics and may differ from run to run; a token's results do not depend on its place in a tile. */
+   the atomics and may differ from run to run; a token's results depend neither on its place in a tile nor on
+   the tile. */
 __global__ __launch_bounds__(SORT_THREADS) void k_lora_sort(const int32_t* adapter_of, int n_tokens, int n_adapters,
                                                             int32_t* order) {
     extern __shared__ int32_t bin[];           /* [n_adapters + 1] */

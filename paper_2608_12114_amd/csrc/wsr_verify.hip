@@ -43,7 +43,7 @@ __device__ __forceinline__ float exp_from(float l, float m, float c) {
 
 __device__ __forceinline__ float temperature_of(const wsr_verify& p, int b) {
     const float t = p.temperature ? p.temperature[b] : 1.f;
-    return t > 0.f ? t : 0.f;
+    return t > 0.f ? fminf(t, 1e30f) : 0.f;       /* the factor of an infinite one would meet infinite differences */
 }
 /* log2 e / T, the factor of exp2; negative for T = 0, where all probability is on one index. */
 __device__ __forceinline__ float factor_of(float t) { return t > 0.f ? LOG2E / t : -1.f; }

@@ -192,3 +192,32 @@ def test_broken_values_reach_the_queries_that_see_them_only(counts, lens, P, H, 
     assert (err <= (u + 1e-4) * mag + u * out.abs() + 64 * 2.0 ** -25 * (1 + mag.amax(-1, keepdim=True)))[whole].all()
     assert ((c.lse.double() - lse).abs() <= 2e-5)[whole].all()
     assert torch.isnan(c.out[~whole][:, :, 3]).all() and not torch.isfinite(c.out[~whole][:, :, 77]).any()
+
+
+@pytest.mark.parametrize("counts,lens", [([1, 1, 1], [300, 1, 1999]), ([5], [2500]), ([3] * 40, [700] * 39 + [3])])
+def test_caches_with_more_room_than_keys(counts, lens):
+    """Parts of the own keys follow the lengths, not the cache's room."""
+    c = Case(counts, lens, 700, 8, 2, 128, torch.bfloat16, seed=21, S=9000)
+    c.run()
+    c.check()
+    tight = Case(counts, lens, 700, 8, 2, 128, torch.bfloat16, seed=21)
+    for name in ("q", "kp", "vp"):
+        getattr(tight, name).copy_(getattr(c, name))
+    tight.k.copy_(c.k[:, :max(lens)]), tight.v.copy_(c.v[:, :max(lens)])
+    tight.run()
+    tight.check()
+
+
+@pytest.mark.parametrize("P", [1, 33, 300, 1000])
+@pytest.mark.parametrize("counts", [[1, 1], [20, 9]])
+def test_an_infinite_value_at_the_end_of_the_prefix(P, counts):
+    """All rows see it: their outputs are that infinity in its channel and nothing else changes."""
+    c = Case(counts, [40, 30], P, 4, 2, 64, torch.float16, seed=22)
+    c.q.mul_(0.25)                                        # so that no probability vanishes
+    want, _, mag = su.attn64(c.q, c.kp, c.vp, c.k, c.v, c.starts, c.lens, c.scale)
+    c.vp[P - 1, :, 7] = float("inf")
+    c.run()
+    assert (c.out[..., 7] == float("inf")).all()
+    u, rest = su.U16[torch.float16], torch.arange(64, device="cuda") != 7
+    bound = (u + 1e-4) * mag + u * want.abs() + 2.0 ** -19 * (1 + mag.amax(-1, keepdim=True))
+    assert ((c.out.double() - want).abs() <= bound)[..., rest].all()

@@ -198,3 +198,32 @@ def test_inner_vectors_of_any_size(size):
     c.mods[0]["x"].mul_(min(size, 1.0) ** 0.15 if size < 1 else 300.0)
     c.run()
     c.check()
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,n,rank", [(500, 5, 24), (333, 20, 12), (200, 9, 64)])
+def test_bits_do_not_depend_on_a_tokens_place(T, n, rank, dt):
+    """The same tokens in another order, so in other tiles beside other adapters, get the same bits."""
+    c = Case([(136, 264)], T, n, rank, dt, seed=13)
+    m = c.mods[0]
+    m["b"][1, ::40, 0] = float("inf")
+    c.run()
+    want, x, y0, ids = m["y"].clone(), m["x"].clone(), m["y0"].clone(), c.ids.clone()
+    for seed in range(3):
+        to = torch.randperm(T, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+        m["x"].copy_(x[to]), m["y0"].copy_(y0[to]), c.ids.copy_(ids[to])
+        m["y"].fill_(float("nan"))
+        c.run()
+        assert torch.equal(m["y"].view(torch.int32), want[to].view(torch.int32))
+
+
+@pytest.mark.parametrize("T", [1, 20, 100])
+def test_an_infinite_weight_gives_infinities(T):
+    """An infinity in the last ranks of a single adapter, whose ranks do not fill the last product."""
+    for rank in (8, 16, 24):
+        c = Case([(64, 64)], T, 1, rank, torch.bfloat16, seed=14)
+        m = c.mods[0]
+        m["b"][0, 5, rank - 1] = float("inf")
+        c.run()
+        assert torch.isinf(m["y"][:, 5]).all()
+        assert torch.isfinite(m["y"][:, torch.arange(64, device="cuda") != 5]).all()

@@ -190,3 +190,16 @@ def test_without_logp_other_stream_and_graph():
         got = c.out.clone()
         c.run()
         assert torch.equal(got, c.out)
+
+
+def test_infinite_temperature_is_even():
+    """All that can be drawn is equally likely; with an infinite logit, that one alone."""
+    c = Case(4, 2, 300, seed=31, temps=(INF, INF))
+    c.target[:, :, 5] = -INF
+    c.target[1, 0, 9] = INF
+    c.run()
+    token, logp = c.out[:, 0].tolist(), c.logp[:, 0].tolist()
+    assert 5 not in c.out.flatten().tolist()
+    for b in (0, 2, 3):
+        assert abs(logp[b] + 5.7004435733906869) < 1e-5, logp       # log 299
+    assert token[1] == 9 and logp[1] == 0

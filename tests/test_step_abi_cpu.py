@@ -124,6 +124,13 @@ def test_attention_refusals(over, st):
     assert L.wsr_prefix_attention(_attn(**over), A, max(need, 1 << 40), None) == st, ws.wsr_step_last_error()
 
 
+def test_attention_row_numbers_fit():
+    """2^20 tokens of 4096 heads on one key head are more rows than are counted in 32 bits."""
+    wide = _attn(n_heads=4096, n_kv_heads=1, n_tokens=1 << 20, q_head_stride=16, out_head_stride=128)
+    assert L.wsr_prefix_attention(wide, A, 1 << 40, None) == SIZE
+    assert wsr.wsr_attn_workspace_bytes(wide) == 0
+
+
 def test_attention_workspace():
     need = wsr.wsr_attn_workspace_bytes(_attn())
     assert L.wsr_prefix_attention(_attn(), A, need - 1, None) == SIZE
