@@ -13,8 +13,8 @@
  *                   row's adapter.
  *   k_lora_expand   (projection, tile, rows): four chunks side by side are the 32 terms of one
  *                   v_mfma_f32_16x16x32; a token's inner vector enters for its own adapter's chunks and as
- *                   zeros for the others; tokens that were put in order have each adapter's chunks begin a product
- *                   of their own, so that a token's sums do not depend on the tile that the order, which is free
+ *                   zeros for the others; for tokens that were put in order each adapter's chunks lie alike in
+ *                   the products, so that a token's sums do not depend on the tile that the order, which is free
  *                   inside an adapter, put it in.  The inner vectors are fp32 (24 bits): they enter as the sum of
  *                   three bf16 terms (24 bits) or of two f16 terms (22 bits, each token's vector scaled by a
  *                   power of two so that its largest entry is near 2^10), products with B exact, sums fp32.
@@ -39,7 +39,9 @@ constexpr int TILE = 64;                       /* tokens of a tile */
 constexpr int WINDOW = 64;                     /* ranks worked on at a time */
 constexpr int BLOCK_K = 256;                   /* elements of K that a workgroup's waves take in turn, 64 each */
 constexpr int SORT_THREADS = 1024;
-constexpr int SHRINK_HELD = 512, EXPAND_HELD = 512;   /* workgroups on the chip at a time: two per CU */
+constexpr int SHRINK_HELD = 512;               /* workgroups on the chip at a time: two per CU */
+/* Waves per SIMD of the second launch, a workgroup per CU each: four for up to 16 tokens, three for 64. */
+constexpr int expand_waves(int token_tiles) { return token_tiles == 1 ? 4 : 3; }
 typedef u32x4 u32x4_any_t __attribute__((aligned(2)));
 typedef u32x2 u32x2_any_t __attribute__((aligned(2)));
 
@@ -89,12 +91,14 @@ struct Tile {
     int32_t list[COLS * (WINDOW / 8)];
     int32_t tok[COLS], id[COLS], rank[COLS];   /* -1: no token, no adapter (or none of its ranks) */
     float scale[COLS];
-    int32_t chunks, mixed, partial;            /* mixed: tokens of more than one adapter; partial: a chunk under 8 ranks */
+    int32_t chunks, partial;                   /* partial: a chunk under 8 ranks */
 };
 
-/* The tile's tokens and the chunks of ranks w0 .. w0 + WINDOW - 1, by the first wave.  FOURS: each adapter's chunks
-   are filled up to a multiple of four with stand-ins of its last. */
-template <bool FOURS, int COLS>
+/* The tile's tokens and the chunks of ranks w0 .. w0 + WINDOW - 1, by the first wave.  PLACED: for
+   tokens that were put in order, an adapter's chunks lie where a step of four divides them alike in every tile:
+   three or more are filled up to a multiple of four with stand-ins of the last and come first, then pairs, then
+   single ones. */
+template <bool PLACED, int COLS>
 __device__ __forceinline__ void make_tile(const LoraCall& c, int tile, int rank, int w0, Tile<COLS>& t) {
     if (threadIdx.x < WAVE) {
         const int lane = threadIdx.x, at = tile * TILE + lane;
@@ -115,23 +119,31 @@ __device__ __forceinline__ void make_tile(const LoraCall& c, int tile, int rank,
             for (int j = 0; j < n; ++j)
                 if (j < lane && __builtin_amdgcn_readlane(id, j) == id) first = false;
         }
-        const int real = first ? (min(max(r - w0, 0), WINDOW) + 7) / 8 : 0, mine = FOURS && c.order ? (real + 3) / 4 * 4 : real;
-        int sum = mine;
+        const int real = first ? (min(max(r - w0, 0), WINDOW) + 7) / 8 : 0;
+        const bool placed = PLACED && c.order;
+        const int mine = placed && real > 2 ? (real + 3) / 4 * 4 : real;
+        int sum = placed && real <= 2 ? 0 : mine;
 #pragma unroll
         for (int k = 1; k < WAVE; k <<= 1) {
             const int o = __shfl_up(sum, k);
             if (lane >= k) sum += o;
         }
+        int all = __builtin_amdgcn_readlane(sum, WAVE - 1), at_list = sum - mine;
+        if (placed) {
+            const uint64_t two = __ballot(real == 2), one = __ballot(real == 1), below = (1ull << lane) - 1;
+            if (real == 2) at_list = all + 2 * __builtin_popcountll(two & below);
+            all += 2 * __builtin_popcountll(two);
+            if (real == 1) at_list = all + __builtin_popcountll(one & below);
+            all += __builtin_popcountll(one);
+        }
         for (int k = 0; k < mine; ++k)
-            t.list[sum - mine + k] = id << 8 | min(k, real - 1) << 4 | (k < real ? min(8, r - w0 - 8 * k) : 0);
-        const int all = __shfl(sum, WAVE - 1);
+            t.list[at_list + k] = id << 8 | min(k, real - 1) << 4 | (k < real ? min(8, r - w0 - 8 * k) : 0);
         if (lane < COLS) {
             t.tok[lane] = tok, t.id[lane] = id, t.rank[lane] = r;
             t.scale[lane] = id >= 0 && c.scales ? c.scales[id] : 1.f;
         }
-        const int adapters = __builtin_popcountll(__ballot(first));
         const bool odd = __ballot(first && r % 8) != 0;
-        if (lane == 0) t.chunks = all, t.mixed = adapters > 1, t.partial = odd;
+        if (lane == 0) t.chunks = all, t.partial = odd;
     }
     __syncthreads();
 }
@@ -403,9 +415,9 @@ __device__ __forceinline__ void make_inner(const LoraMod& d, const LoraCall& c, 
 }
 
 /* A wave's 16 RW rows of a unit against the tile's tokens, U steps of four chunks at a time.  STREAM: outputs are
-   stored past the caches. */
+   loaded and stored past the caches. */
 template <int FMT, int TT, int RW, bool STREAM, int N>
-__global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_lora_expand(LoraTable<N> tab, LoraCall c) {
+__global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(expand_waves(TT)))) void k_lora_expand(LoraTable<N> tab, LoraCall c) {
     constexpr int COLS = 16 * TT, ROWS = LW * 16 * RW, U = TT == 1 ? 4 : 2, NTERM = terms<FMT>();
     typedef Inner<FMT, COLS> I;
     __shared__ Tile<COLS> t;
@@ -439,7 +451,8 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
                     for (int i = 0; i < RW; ++i) {
                         const int tok = t.tok[16 * j + out_col(i)];
                         const float* src = (const float*)((const char*)d.y0 + (tok < 0 ? t.tok[0] : tok) * d.y0_stride);
-                        y0[i][j] = *(const f4_any_t*)(src + i0 + out_row(i));
+                        if constexpr (STREAM) y0[i][j] = __builtin_nontemporal_load((const f4_any_t*)(src + i0 + out_row(i)));
+                        else y0[i][j] = *(const f4_any_t*)(src + i0 + out_row(i));
                     }
             }
             if (t.chunks == 0) break;          /* no adapter reaches this window or a later one */
@@ -453,9 +466,6 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
             for (int j = 0; j < TT; ++j) id[j] = t.id[16 * j + col];
             const bool partial = __builtin_amdgcn_readfirstlane(t.partial);
             const int chunks = __builtin_amdgcn_readfirstlane(t.chunks);
-            /* zero times an infinity or NaN of one adapter's weights would reach the tokens of the others, and in a
-               stand-in make NaN of an infinity */
-            const bool watch = c.order || __builtin_amdgcn_readfirstlane(t.mixed) || chunks % 4;
             int64_t row[RW];
 #pragma unroll
             for (int i = 0; i < RW; ++i) row[i] = min(i0 + 16 * i + col, d.M - 1) * d.rank * 2;
@@ -484,16 +494,16 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
                         for (int i = 0; i < RW; ++i) b[u][i] = load_weights<TT == 1>(p[u] + row[i]);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                /* steps with infinities or NaN go chunk by chunk, a chunk's sums taken over by its own tokens only */
+                /* zero times an infinity or NaN of one adapter's weights would reach the tokens of the others, and a second
+                   term of the other sign make NaN of an infinity: such steps go adapter by adapter, its sums taken over
+                   by its own tokens only and its infinities and NaN multiplied with the first terms */
                 uint32_t apart = 0;
-                if (watch) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        uint32_t bad = 0;
+                for (int u = 0; u < U; ++u) {
+                    uint32_t bad = 0;
 #pragma unroll
-                        for (int i = 0; i < RW; ++i) bad |= not_finite<FMT>(b[u][i]);
-                        apart |= __ballot(bad != 0) ? 1u << u : 0u;
-                    }
+                    for (int i = 0; i < RW; ++i) bad |= not_finite<FMT>(b[u][i]);
+                    apart |= __ballot(bad != 0) ? 1u << u : 0u;
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -518,11 +528,13 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
                         } else {
 #pragma unroll 1
                             for (int o = 0; o < 4; ++o) {
-                                const bool mine = id[j] >= 0 && id[j] == __shfl(adapter[u], 16 * o);
+                                const int its = __shfl(adapter[u], 16 * o);
+                                if (o && its == __shfl(adapter[u], 16 * (o - 1))) continue;
+                                const bool mine = id[j] >= 0 && id[j] == its;
 #pragma unroll
                                 for (int i = 0; i < RW; ++i) {
                                     f4_t s = acc[i][j];
-                                    u32x4 w = g == o ? b[u][i] : wsr::zero4();
+                                    u32x4 w = adapter[u] == its ? b[u][i] : wsr::zero4();
                                     asm volatile("" : "+v"(w));          /* or the next line's registers are held all along */
 #pragma unroll
                                     for (int k = 0; k < NTERM; ++k) {
@@ -581,6 +593,87 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(2))) void k_
                 }
             }
         }
+    }
+}
+
+/* Few tokens over few projections, in one launch: a workgroup takes LT rows of a projection, works out the inner
+   vectors for itself (a wave four rows of A at a time, on the vector ALUs) and gives each thread a row of B, whose
+   loads are under way before. */
+constexpr int SMALL_RANK = WINDOW;
+template <int FMT, int N>
+__global__ __launch_bounds__(LT) void k_lora_small(LoraTable<N> tab, LoraCall c) {
+    constexpr int RJ = 4, U = 4, PIECES = SMALL_RANK / 8;
+    __shared__ float v[2][SMALL_RANK];
+    const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block();
+    const int m = mod_of(tab, blockIdx.x);
+    const LoraMod& d = tab.mod[m];
+    const int64_t row = (int64_t)(blockIdx.x - tab.first[m]) * LT + threadIdx.x;
+    int half = 0;
+    for (int t = 0; t < c.n_tokens; ++t) {
+        int id = c.adapter_of[t], r = 0;
+        if (id >= 0 && id < c.n_adapters) r = c.ranks ? min(max(c.ranks[id], 0), d.rank) : d.rank;
+        if (r == 0 && d.y0 == d.y) continue;
+        float* y = (float*)((char*)d.y + t * d.y_stride) + row;
+        float s = d.y0 && row < d.M ? ((const float*)((const char*)d.y0 + t * d.y0_stride))[row] : 0.f;
+        if (r > 0) {
+            const char* br = (const char*)d.b + id * d.b_stride + min(row, d.M - 1) * d.rank * 2;
+            u32x4 b[PIECES];
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) b[p] = 8 * p < r ? load_chunk_row(br + 16 * p, min(8, r - 8 * p)) : wsr::zero4();
+            const char *ar = (const char*)d.a + id * d.a_stride, *xr = (const char*)d.x + t * d.x_stride;
+            const float scale = c.scales ? c.scales[id] : 1.f;
+            for (int j = wave * RJ; j < r; j += LW * RJ) {
+                const char* a[RJ];
+                float acc[RJ] = {};
+#pragma unroll
+                for (int i = 0; i < RJ; ++i) a[i] = ar + min(j + i, r - 1) * d.K * 2;
+                auto step = [&](auto steps, int64_t k) {
+                    constexpr int S = decltype(steps)::value;
+                    u32x4 x[S], w[S][RJ];
+#pragma unroll
+                    for (int u = 0; u < S; ++u) {
+                        x[u] = *(const u32x4*)(xr + (k + u * WAVE * 8) * 2);
+#pragma unroll
+                        for (int i = 0; i < RJ; ++i) w[u][i] = *(const u32x4*)(a[i] + (k + u * WAVE * 8) * 2);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int u = 0; u < S; ++u) {
+                        float xv[8];
+                        unpack8<FMT>(x[u], xv);
+#pragma unroll
+                        for (int i = 0; i < RJ; ++i) {
+                            float wv[8];
+                            unpack8<FMT>(w[u][i], wv);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) acc[i] = fmaf(wv[e], xv[e], acc[i]);
+                        }
+                    }
+                };
+                int64_t k = lane * 8;
+                for (; k + (U - 1) * WAVE * 8 < d.K; k += U * WAVE * 8) step(std::integral_constant<int, U>{}, k);
+                for (; k < d.K; k += WAVE * 8) step(std::integral_constant<int, 1>{}, k);
+#pragma unroll
+                for (int i = 0; i < RJ; ++i) {
+                    const float sum = wsr::wave_sum(acc[i]);
+                    if (lane == 0 && j + i < r) v[half][j + i] = sum * scale;
+                }
+            }
+            __syncthreads();                   /* the next vector goes to the other half */
+            float dot = 0.f;
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                if (8 * p >= r) break;
+                float bv[8];
+                unpack8<FMT>(b[p], bv);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (8 * p + e < r) dot = fmaf(bv[e], v[half][8 * p + e], dot);
+            }
+            s += dot;
+            half ^= 1;
+        }
+        if (row < d.M) *y = s;
     }
 }
 
@@ -645,6 +738,7 @@ static int least_span(const wsr_lora* mods, int32_t n, int32_t n_tokens) {
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 static size_t order_bytes(int32_t n_tokens) { return n_tokens <= TILE ? 0 : up256(4 * (size_t)n_tokens); }
 constexpr int TABLE_MAX = 224;
+constexpr int64_t SMALL_BYTES = 512 << 10, SMALL_UNITS = 512;
 
 /* Runs of projections that one pair of launches takes: of one type, at most a table's length. */
 static int32_t run_of(const wsr_lora* mods, int32_t n) {
@@ -700,7 +794,7 @@ static hipError_t launch_expand(LoraTable<N>& tab, const LoraCall& c, hipStream_
     }
     if (units == 0) return hipSuccess;
     tab.units = (int32_t)units;
-    hipLaunchKernelGGL((k_lora_expand<FMT, TT, RW, STREAM, N>), dim3(grid_of(units, c.tiles, EXPAND_HELD)), dim3(LT), 0, s, tab, c);
+    hipLaunchKernelGGL((k_lora_expand<FMT, TT, RW, STREAM, N>), dim3(grid_of(units, c.tiles, 256 * expand_waves(TT))), dim3(LT), 0, s, tab, c);
     return hipGetLastError();
 }
 
@@ -715,12 +809,34 @@ static hipError_t launch_pair(LoraTable<N>& tab, const LoraCall& c, bool one, hi
     else hipLaunchKernelGGL((k_lora_shrink<FMT, TT, 4, N>), grid, dim3(LT), 0, s, tab, c);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    /* units of 64 rows instead of 256 where the latter would be fewer than places on the chip */
+    /* units of 64 rows instead of 128 where the latter would leave half of the chip's places empty */
     if constexpr (TT == 1)
-        if (rows / 256 < EXPAND_HELD) return launch_expand<FMT, 1, 1, false, N>(tab, c, s);
-    if constexpr (TT > 1)
-        if (c.stream) return launch_expand<FMT, TT, 4, true, N>(tab, c, s);
-    return launch_expand<FMT, TT, 4, false, N>(tab, c, s);
+        if (rows / 256 < 512) return launch_expand<FMT, 1, 1, false, N>(tab, c, s);
+    if (c.stream) return launch_expand<FMT, TT, 2, true, N>(tab, c, s);
+    return launch_expand<FMT, TT, 2, false, N>(tab, c, s);
+}
+
+/* Whether one launch does: every workgroup reads all of the tokens' rows of A, so they are to be short, the
+   workgroups few and the tokens few. */
+static bool is_small(const LoraMod* mods, int n, int32_t n_tokens) {
+    int64_t units = 0;
+    for (int i = 0; i < n; ++i) {
+        if (mods[i].rank > SMALL_RANK || n_tokens * mods[i].rank * mods[i].K * 2 > SMALL_BYTES) return false;
+        units += (mods[i].M + LT - 1) / LT;
+    }
+    return units <= SMALL_UNITS;
+}
+
+template <int FMT, int N>
+static hipError_t launch_small(LoraTable<N>& tab, const LoraCall& c, hipStream_t s) {
+    int64_t units = 0;
+    for (int i = 0; i < tab.n; ++i) {
+        tab.first[i] = (int32_t)units;
+        units += (tab.mod[i].M + LT - 1) / LT;
+    }
+    if (units == 0) return hipSuccess;
+    hipLaunchKernelGGL((k_lora_small<FMT, N>), dim3((unsigned)units), dim3(LT), 0, s, tab, c);
+    return hipGetLastError();
 }
 
 template <int N>
@@ -729,6 +845,9 @@ static hipError_t launch_table(const LoraMod* mods, int n, int fmt, int64_t bloc
     tab.n = n;
     tab.units = (int32_t)blocks;
     std::copy(mods, mods + n, tab.mod);
+    if constexpr (N == 8)
+        if (is_small(mods, n, c.n_tokens))
+            return fmt == WSR_F16 ? launch_small<WSR_F16, N>(tab, c, s) : launch_small<WSR_BF16, N>(tab, c, s);
     const bool few = c.n_tokens <= 16;
     if (fmt == WSR_F16) return few ? launch_pair<WSR_F16, 1, N>(tab, c, one, s) : launch_pair<WSR_F16, 4, N>(tab, c, one, s);
     return few ? launch_pair<WSR_BF16, 1, N>(tab, c, one, s) : launch_pair<WSR_BF16, 4, N>(tab, c, one, s);

@@ -31,8 +31,11 @@ struct Stat {
     int32_t pad;
 };
 struct Best {
-    float w, p;      /* largest residual score and largest plain score */
-    int32_t wi, pi;
+    float w;         /* the largest score of a chunk */
+    int32_t wi;      /* its index */
+    float p;         /* the same of plain scores, without the draft's probabilities */
+    int32_t pi;
+    float wl, pl;    /* their logits */
 };
 
 __device__ __forceinline__ float no_nan(float v) { return v == v ? v : NEG_INF; }
@@ -80,11 +83,37 @@ __device__ __forceinline__ void load_chunk(const float* row, int64_t at, int64_t
 __device__ __forceinline__ void better(float& w, int& i, float w2, int i2) {
     if (w2 > w || (w2 == w && i2 < i)) w = w2, i = i2;
 }
+__device__ __forceinline__ void better(Best& a, const Best& b) {
+    if (b.w > a.w || (b.w == a.w && b.wi < a.wi)) a.w = b.w, a.wi = b.wi, a.wl = b.wl;
+    if (b.p > a.p || (b.p == a.p && b.pi < a.pi)) a.p = b.p, a.pi = b.pi, a.pl = b.pl;
+}
 /* The largest w of a wave and the lowest index that has it. */
 __device__ __forceinline__ void wave_best(float& w, int& i) {
     const float top = wave_max(w);
     i = wave_min(w == top ? i : 0x7fffffff);
     w = top;
+}
+/* And what belongs to that index. */
+__device__ __forceinline__ void wave_best(float& w, int& i, float& l) {
+    const int mine = i;
+    wave_best(w, i);
+    l = __shfl(l, __builtin_ctzll(__ballot(mine == i)));
+}
+/* Words that workgroups of different XCDs pass to one another: stored to and loaded from where all of them see
+   them, past the caches that they do not share. */
+struct Words {
+    uint64_t w[3];
+};
+__device__ __forceinline__ void pass_on(Words* to, const Best& b) {
+    const Words o = __builtin_bit_cast(Words, b);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) __hip_atomic_store(&to->w[i], o.w[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ Best passed(const Words* from) {
+    Words o;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) o.w[i] = __hip_atomic_load(&from->w[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return __builtin_bit_cast(Best, o);
 }
 
 template <int VU>
@@ -125,14 +154,21 @@ __global__ __launch_bounds__(VT) void k_verify_stats(wsr_verify p, Stat* stats, 
     if (threadIdx.x == 0) stats[((int64_t)b * rows + r) * chunks + c] = Stat{m, s, at, 0};
 }
 
-/* A row's statistics from its chunks, by sixteen lanes (lane j takes chunks j, j + 16, ...). */
+/* A row's statistics from its chunks, by sixteen lanes (lane j takes chunks j, j + 16, ..., four of them loaded at
+   a time). */
 __device__ __forceinline__ Stat join_row(const Stat* st, int chunks, float k, int j) {
     float m = NEG_INF, s = 0.f;
     int at = 0x7fffffff;
-    for (int c = j; c < chunks; c += 16) {
-        const Stat o = st[c];
-        if (o.m > m) s = s * (m > NEG_INF ? exp_from(m, o.m, k) : 0.f) + o.s, m = o.m, at = o.at;
-        else if (o.m > NEG_INF) s += o.s * exp_from(o.m, m, k);
+    for (int c = j; c < chunks; c += 64) {
+        Stat o[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = st[min(c + 16 * e, chunks - 1)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (c + 16 * e >= chunks) break;
+            if (o[e].m > m) s = s * (m > NEG_INF ? exp_from(m, o[e].m, k) : 0.f) + o[e].s, m = o[e].m, at = o[e].at;
+            else if (o[e].m > NEG_INF) s += o[e].s * exp_from(o[e].m, m, k);
+        }
     }
     const float top = row_max(m);
     at = row_min(m == top ? at : 0x7fffffff);
@@ -156,12 +192,12 @@ __device__ __forceinline__ float log_prob(float l, int i, const Stat& st, float 
 constexpr int MAX_ROWS = 2 * 63 + 1;
 
 template <int VU>
-__global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* stats, Best* best, uint32_t* done, int rows,
+__global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* stats, Words* best, uint32_t* done, int rows,
                                                     int chunks) {
     constexpr int CHUNK = VT * VU * 4;
     __shared__ Stat all[MAX_ROWS];
-    __shared__ float sw[VT / WAVE], sp[VT / WAVE];
-    __shared__ int swi[VT / WAVE], spi[VT / WAVE], verdict, last;
+    __shared__ Best bests[VT / WAVE];
+    __shared__ int verdict, last;
     const int c = blockIdx.x % chunks, b = blockIdx.x / chunks, wave = threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
     const int count = count_of(p, b), n = p.n_drafts;
     const float t = temperature_of(p, b), k = factor_of(t);
@@ -170,16 +206,16 @@ __global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* st
     load_chunk<VU>((const float*)((const char*)p.noise + b * p.noise_seq_stride), (int64_t)c * CHUNK, p.vocab, 1.f, z);
     int x = -1;
     float u = 0.f, lt = NEG_INF, ld = NEG_INF;
-    if (wave == 0 && lane < count) {
+    if (wave == 0 && lane < n) {
         x = p.tokens[(int64_t)b * n + lane];
         u = p.uniform[(int64_t)b * n + lane];
+        if (lane >= count) x = -1;
         if (x >= 0 && x < p.vocab) {
             lt = row_of(p, b, lane, count)[x];
             if (p.draft) ld = row_of(p, b, n + 1 + lane, count)[x];
         }
     }
     for (int r = threadIdx.x / 16; r < rows; r += VT / 16) {
-        if (!row_of(p, b, r, count)) continue;
         const Stat st = join_row(stats + ((int64_t)b * rows + r) * chunks, chunks, k, threadIdx.x % 16);
         if (threadIdx.x % 16 == 0) all[r] = st;
     }
@@ -217,7 +253,7 @@ __global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* st
     const Stat sq = qrow ? all[n + 1 + a] : Stat{0.f, 1.f, 0, 0};
     const int point = residual && !p.draft ? p.tokens[(int64_t)b * n + a] : -1;
     const float ip = 1.f / st.s, iq = 1.f / sq.s;
-    float bw = 0.f, bp = 0.f;
+    float bw = 0.f, bp = 0.f, bwl = 0.f, bpl = 0.f;
     int bwi = 0x7fffffff, bpi = 0x7fffffff;
 #pragma unroll
     for (int e = 0; e < VU; ++e)
@@ -229,37 +265,33 @@ __global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* st
             if (qrow) w = pv - prob(q[e][j], i, sq, iq, k);
             else if (i == point) w = pv - 1.f;
             const float rn = __builtin_amdgcn_rcpf(z[e][j]);
-            if (w > 0.f && w * rn > bw) bw = w * rn, bwi = i;
-            if (pv * rn > bp) bp = pv * rn, bpi = i;
+            if (w > 0.f && w * rn > bw) bw = w * rn, bwi = i, bwl = v[e][j];
+            if (pv * rn > bp) bp = pv * rn, bpi = i, bpl = v[e][j];
         }
-    wave_best(bw, bwi);
-    wave_best(bp, bpi);
-    if (lane == 0) sw[wave] = bw, swi[wave] = bwi, sp[wave] = bp, spi[wave] = bpi;
+    wave_best(bw, bwi, bwl);
+    wave_best(bp, bpi, bpl);
+    if (lane == 0) bests[wave] = Best{bw, bwi, bp, bpi, bwl, bpl};
     __syncthreads();
     if (threadIdx.x == 0) {
+        Best o = bests[0];
 #pragma unroll
-        for (int w = 1; w < VT / WAVE; ++w) better(bw, bwi, sw[w], swi[w]), better(bp, bpi, sp[w], spi[w]);
-        best[(int64_t)b * chunks + c] = Best{bw, bp, bwi, bpi};
-        /* releases this workgroup's best to whichever counts last; only that one acquires (with an acquire in all
-           of them, which empties caches each time, the race of 64 sequences took 41 us, so 33) */
-        last = __hip_atomic_fetch_add(&done[b], 1u, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)chunks - 1;
-        if (last) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+        for (int w = 1; w < VT / WAVE; ++w) better(o, bests[w]);
+        pass_on(&best[(int64_t)b * chunks + c], o);
+        /* counted once the words above have arrived (a release and an acquire, which write back and empty caches that
+           hold nothing of this, made the race of 64 sequences take RELEASED us, so PASSED) */
+        wait_loads<0>();
+        last = __hip_atomic_fetch_add(&done[b], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)chunks - 1;
     }
     __syncthreads();
     if (!last || wave) return;
-    float w = 0.f, f = 0.f;
-    int wi = 0x7fffffff, fi = 0x7fffffff;
-    for (int i = lane; i < chunks; i += WAVE) {
-        const Best o = best[(int64_t)b * chunks + i];
-        better(w, wi, o.w, o.wi);
-        better(f, fi, o.p, o.pi);
-    }
-    wave_best(w, wi);
-    wave_best(f, fi);
+    Best o{0.f, 0x7fffffff, 0.f, 0x7fffffff, 0.f, 0.f};
+    for (int i = lane; i < chunks; i += WAVE) better(o, passed(&best[(int64_t)b * chunks + i]));
+    wave_best(o.w, o.wi, o.wl);
+    wave_best(o.p, o.pi, o.pl);
     if (lane) return;
-    const int token = w > 0.f ? wi : f > 0.f ? fi : -1;
+    const int token = o.w > 0.f ? o.wi : o.p > 0.f ? o.pi : -1;
     p.out[(int64_t)b * (n + 1) + a] = token;
-    if (p.logp) p.logp[(int64_t)b * (n + 1) + a] = token < 0 ? NEG_INF : log_prob(prow[token], token, st, t);
+    if (p.logp) p.logp[(int64_t)b * (n + 1) + a] = token < 0 ? NEG_INF : log_prob(o.w > 0.f ? o.wl : o.pl, token, st, t);
 }
 
 struct VerifyPlan {
@@ -276,7 +308,7 @@ static VerifyPlan plan_of(const wsr_verify& p) {
     v.chunks = (int)(v.fine ? (p.vocab + VT * 8 - 1) / (VT * 8) : wide);
     const size_t pairs = (size_t)p.n_seqs * v.chunks;
     v.best_at = (pairs * v.rows * sizeof(Stat) + 255) / 256 * 256;
-    v.done_at = v.best_at + (pairs * sizeof(Best) + 255) / 256 * 256;
+    v.done_at = v.best_at + (pairs * sizeof(Words) + 255) / 256 * 256;
     v.bytes = v.done_at + (size_t)p.n_seqs * sizeof(uint32_t);
     return v;
 }
@@ -286,7 +318,7 @@ size_t verify_workspace(const wsr_verify& p) { return plan_of(p).bytes; }
 template <int VU>
 static hipError_t launch_two(const wsr_verify& p, const VerifyPlan& v, char* ws, hipStream_t s) {
     Stat* stats = reinterpret_cast<Stat*>(ws);
-    Best* best = reinterpret_cast<Best*>(ws + v.best_at);
+    Words* best = reinterpret_cast<Words*>(ws + v.best_at);
     uint32_t* done = reinterpret_cast<uint32_t*>(ws + v.done_at);
     const int64_t blocks = (int64_t)p.n_seqs * v.rows * v.chunks;
     if (blocks > INT32_MAX) return hipErrorInvalidValue;

@@ -219,8 +219,8 @@ def test_bits_do_not_depend_on_a_tokens_place(T, n, rank, dt):
 
 @pytest.mark.parametrize("T", [1, 20, 100])
 def test_an_infinite_weight_gives_infinities(T):
-    """An infinity in the last ranks of a single adapter, whose ranks do not fill the last product."""
-    for rank in (8, 16, 24):
+    """An infinity in the last ranks of a single adapter, whose ranks may leave the last product part empty."""
+    for rank in (8, 16, 24, 32):
         c = Case([(64, 64)], T, 1, rank, torch.bfloat16, seed=14)
         m = c.mods[0]
         m["b"][0, 5, rank - 1] = float("inf")
