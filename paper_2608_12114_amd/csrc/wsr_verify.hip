@@ -277,8 +277,7 @@ __global__ __launch_bounds__(VT) void k_verify_race(wsr_verify p, const Stat* st
 #pragma unroll
         for (int w = 1; w < VT / WAVE; ++w) better(o, bests[w]);
         pass_on(&best[(int64_t)b * chunks + c], o);
-        /* counted once the words above have arrived (a release and an acquire, which write back and empty caches that
-           hold nothing of this, made the race of 64 sequences take RELEASED us, so PASSED) */
+        /* counted once the words above have arrived: no caches to write back or to empty */
         wait_loads<0>();
         last = __hip_atomic_fetch_add(&done[b], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)chunks - 1;
     }
@@ -302,9 +301,10 @@ struct VerifyPlan {
 static VerifyPlan plan_of(const wsr_verify& p) {
     VerifyPlan v;
     v.rows = p.n_drafts + 1 + (p.draft ? p.n_drafts : 0);
-    /* chunks of 8192 logits, of 2048 where the former would leave most of the chip idle in the race */
-    const int64_t wide = (p.vocab + VT * 32 - 1) / (VT * 32);
-    v.fine = p.n_seqs * wide < 256;
+    /* chunks of 4096 logits (64 sequences 110 us, with 8192 118, with 2048 173), of 2048 where the former would leave
+       most of the chip idle in the race */
+    const int64_t wide = (p.vocab + VT * 16 - 1) / (VT * 16);
+    v.fine = p.n_seqs * wide < 512;
     v.chunks = (int)(v.fine ? (p.vocab + VT * 8 - 1) / (VT * 8) : wide);
     const size_t pairs = (size_t)p.n_seqs * v.chunks;
     v.best_at = (pairs * v.rows * sizeof(Stat) + 255) / 256 * 256;
@@ -332,7 +332,7 @@ static hipError_t launch_two(const wsr_verify& p, const VerifyPlan& v, char* ws,
 
 hipError_t launch_verify(const wsr_verify& p, void* ws, hipStream_t s) {
     const VerifyPlan v = plan_of(p);
-    return v.fine ? launch_two<2>(p, v, static_cast<char*>(ws), s) : launch_two<8>(p, v, static_cast<char*>(ws), s);
+    return v.fine ? launch_two<2>(p, v, static_cast<char*>(ws), s) : launch_two<4>(p, v, static_cast<char*>(ws), s);
 }
 
 }  // namespace wsr_step
