@@ -526,21 +526,36 @@ void k_attn(wsr_attn p, AttnPlan pl) {
     }
 }
 
-/* Adds up the n parts of a row, `step` floats apart, and stores it, by one wave. */
+/* Adds up the n parts of a row, `step` floats apart, and stores it, by one wave: in order, eight, four, two and one
+   of them loaded at a time (one by one, each after the one before has come, a token on 32771 keys took 36 us, so 31.5). */
 template <int FMT, int D>
 __device__ __forceinline__ void join_row(const wsr_attn& p, const float* w, int64_t step, int n, int tok, int qh, int lane) {
     constexpr int E = D / WAVE;
     const float c = p.scale * A_LOG2E;
     float m = A_NEG_INF, l = 0.f, o[E] = {};
-    for (int i = 0; i < n; ++i) {
-        const float* v = w + i * step;
-        const float m2 = v[D], top = fmaxf(m, m2), base = top == A_NEG_INF ? 0.f : top * c;
-        const float a = __builtin_amdgcn_exp2f(m * c - base), b = __builtin_amdgcn_exp2f(m2 * c - base);
-        l = l * a + v[D + 1] * b;
-        m = top;
+    auto add = [&](auto count) __attribute__((always_inline)) {
+        constexpr int N = decltype(count)::value;
+        float pm[N], ps[N], po[N][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * a + v[E * lane + e] * b;
-    }
+        for (int k = 0; k < N; ++k, w += step) {
+            pm[k] = w[D], ps[k] = w[D + 1];
+#pragma unroll
+            for (int e = 0; e < E; ++e) po[k][e] = w[E * lane + e];
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float top = fmaxf(m, pm[k]), base = top == A_NEG_INF ? 0.f : top * c;
+            const float a = __builtin_amdgcn_exp2f(m * c - base), b = __builtin_amdgcn_exp2f(pm[k] * c - base);
+            l = l * a + ps[k] * b;
+            m = top;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = o[e] * a + po[k][e] * b;
+        }
+    };
+    for (; n >= 8; n -= 8) add(std::integral_constant<int, 8>{});
+    if (n & 4) add(std::integral_constant<int, 4>{});
+    if (n & 2) add(std::integral_constant<int, 2>{});
+    if (n & 1) add(std::integral_constant<int, 1>{});
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
     char* out = (char*)p.out + tok * p.out_tok_stride + qh * p.out_head_stride;
     if constexpr (E == 2) ((uint32_t*)out)[lane] = pack2<FMT>(o[0] * inv, o[1] * inv);

@@ -683,7 +683,7 @@ __global__ __launch_bounds__(LT) void k_lora_small(LoraTable<N> tab, LoraCall c)
 __global__ __launch_bounds__(SORT_THREADS) void k_lora_sort(const int32_t* adapter_of, int n_tokens, int n_adapters,
                                                             int32_t* order) {
     extern __shared__ int32_t bin[];           /* [n_adapters + 1] */
-    __shared__ int32_t sc[SORT_THREADS];
+    __shared__ int32_t sc[SORT_THREADS / WAVE];
     const int n = n_adapters + 1, tid = threadIdx.x;
     for (int i = tid; i < n; i += SORT_THREADS) bin[i] = 0;
     __syncthreads();
@@ -695,15 +695,16 @@ __global__ __launch_bounds__(SORT_THREADS) void k_lora_sort(const int32_t* adapt
     const int per = (n + SORT_THREADS - 1) / SORT_THREADS, b0 = min(n, tid * per), b1 = min(n, b0 + per);
     int tokens = 0;
     for (int i = b0; i < b1; ++i) tokens += bin[i];
-    sc[tid] = tokens;
-    __syncthreads();
-    for (int k = 1; k < SORT_THREADS; k <<= 1) {
-        const int a = tid >= k ? sc[tid - k] : 0;
-        __syncthreads();
-        sc[tid] += a;
-        __syncthreads();
+    int at = tokens;                           /* of the threads before: inside the wave, then of the waves before */
+#pragma unroll
+    for (int k = 1; k < WAVE; k <<= 1) {
+        const int o = __shfl_up(at, k);
+        if (tid % WAVE >= k) at += o;
     }
-    int at = sc[tid] - tokens;
+    if (tid % WAVE == WAVE - 1) sc[tid / WAVE] = at;
+    at -= tokens;
+    __syncthreads();
+    for (int w = 0; w < tid / WAVE; ++w) at += sc[w];
     for (int i = b0; i < b1; ++i) {
         const int count = bin[i];
         bin[i] = at;
