@@ -6,7 +6,7 @@
  * Tokens go in tiles of up to 64; more than 64 are first put in the order of their adapters by a kernel
  * of one workgroup.  A tile's work is a list of chunks, eight ranks of one adapter each, over all adapters
  * that its tokens have: whatever the adapters' ranks and however many tokens share one, each chunk's weights
- * are read once per tile.  Two launches over all projections:
+ * are read once per tile.  Two launches over all projections (few tokens over short ones take one, k_lora_small):
  *
  *   k_lora_shrink   (tile, span of the projections' K laid end to end): rows of A from two chunks at a time
  *                   against 16 tokens on v_mfma_f32_16x16x32; a span's sum is stored where the token has the
@@ -20,8 +20,11 @@
  *                   power of two so that its largest entry is near 2^10), products with B exact, sums fp32.
  *                   Rounding them to one 16-bit term would leave errors of 2^-9 in the fp32 outputs.
  *
- * Decode is bound by reading the adapters (2 (K + M) rank bytes each), prompts by reading and
- * writing the outputs (8 M bytes per token).
+ * Decode is bound by reading the adapters (2 (K + M) rank bytes each): 16 tokens of 14 adapters of 16 ranks over
+ * the 8B model, 1.22 GB, take 258 us, 4.7 TB/s (the first launch 95 us at 5.4, the second at 4.5, whose outputs, two
+ * streams beside the weights', cost it 60 us).  Prompts are bound by reading and writing the outputs (8 M bytes per
+ * token): 2055 tokens of five adapters of 64 ranks over two 14336 x 4096 projections, 526 MB, take 153 us; without
+ * the products the second launch alone streams for 100 of them.
  */
 #include <hip/hip_runtime.h>
 
@@ -40,7 +43,9 @@ constexpr int WINDOW = 64;                     /* ranks worked on at a time */
 constexpr int BLOCK_K = 256;                   /* elements of K that a workgroup's waves take in turn, 64 each */
 constexpr int SORT_THREADS = 1024;
 constexpr int SHRINK_HELD = 512;               /* workgroups on the chip at a time: two per CU */
-/* Waves per SIMD of the second launch, a workgroup per CU each: four for up to 16 tokens, three for 64. */
+/* Waves per SIMD of the second launch, a workgroup per CU each: four for up to 16 tokens, three for 64, with units
+   of 128 rows (with two, and units of 256 rows, 201 tokens of 31 adapters took 239 us, so 210, 49 of 30 124 and 118;
+   with four for 64 tokens the registers spill, and both lose a fifth). */
 constexpr int expand_waves(int token_tiles) { return token_tiles == 1 ? 4 : 3; }
 typedef u32x4 u32x4_any_t __attribute__((aligned(2)));
 typedef u32x2 u32x2_any_t __attribute__((aligned(2)));
@@ -598,7 +603,8 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(expand_waves
 
 /* Few tokens over few projections, in one launch: a workgroup takes LT rows of a projection, works out the inner
    vectors for itself (a wave four rows of A at a time, on the vector ALUs) and gives each thread a row of B, whose
-   loads are under way before. */
+   loads are under way before.  Bound by one pass of latency: 1 token, 4096 x 4096, 16 ranks 6.1 us in a graph, 10.2
+   in two launches. */
 constexpr int SMALL_RANK = WINDOW;
 template <int FMT, int N>
 __global__ __launch_bounds__(LT) void k_lora_small(LoraTable<N> tab, LoraCall c) {
@@ -739,7 +745,7 @@ static int least_span(const wsr_lora* mods, int32_t n, int32_t n_tokens) {
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 static size_t order_bytes(int32_t n_tokens) { return n_tokens <= TILE ? 0 : up256(4 * (size_t)n_tokens); }
 constexpr int TABLE_MAX = 224;
-constexpr int64_t SMALL_BYTES = 512 << 10, SMALL_UNITS = 512;
+constexpr int64_t SMALL_BYTES = 512 << 10, SMALL_UNITS = 512, SMALL_TOKENS = 3;
 
 /* Runs of projections that one pair of launches takes: of one type, at most a table's length. */
 static int32_t run_of(const wsr_lora* mods, int32_t n) {
@@ -818,8 +824,10 @@ static hipError_t launch_pair(LoraTable<N>& tab, const LoraCall& c, bool one, hi
 }
 
 /* Whether one launch does: every workgroup reads all of the tokens' rows of A, so they are to be short, the
-   workgroups few and the tokens few. */
+   workgroups few and the tokens, which go one after the other, few (1 token over three projections of up to 448 KiB of A, 168 workgroups, 9.1 us, in
+   two launches 12.3; 3 tokens over 384 KiB 13.3 and 12.9, where the host's launch is saved still; 1 MiB 26 and 14). */
 static bool is_small(const LoraMod* mods, int n, int32_t n_tokens) {
+    if (n_tokens > SMALL_TOKENS) return false;
     int64_t units = 0;
     for (int i = 0; i < n; ++i) {
         if (mods[i].rank > SMALL_RANK || n_tokens * mods[i].rank * mods[i].K * 2 > SMALL_BYTES) return false;
@@ -886,9 +894,8 @@ hipError_t launch_lora(const wsr_lora* mods, int32_t n, int32_t n_tokens, const 
            the rounds are spread over what is left */
         const int least = least_span(mods + i, k, n_tokens);
         c.slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, 8 / least));
-        /* outputs larger than the chip's second-level caches are gone from them before they are read again (779 tokens
-           over six layers of four projections 283 us, past the caches 265; 49 tokens over four layers of the 8B
-           model 126 and 121) */
+        /* outputs larger than the chip's second-level caches are gone from them before they are read again: loaded and
+           stored past them (16 tokens over the 8B model 277 us, so 258; 2055 prompt tokens 160 and 154) */
         int64_t rows = 0;
         for (int32_t j = i; j < i + k; ++j) rows += mods[j].M;
         c.stream = rows * n_tokens * 4 >= 32 << 20;

@@ -227,3 +227,43 @@ def test_an_infinite_weight_gives_infinities(T):
         c.run()
         assert torch.isinf(m["y"][:, 5]).all()
         assert torch.isfinite(m["y"][:, torch.arange(64, device="cuda") != 5]).all()
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,n,rank,ranks", [(1, 2, 64, None), (5, 3, 33, [33, 7, 0]), (16, 16, 16, None), (16, 5, 100, [100, 64, 65, 1, 99]),
+                                            (7, 2, 24, None)])
+def test_few_tokens_over_long_rows(T, n, rank, ranks, dt):
+    """Rows of A too long for the form of one launch; whole and odd numbers of rows, tokens without an adapter."""
+    c = Case([(131, 16392), (640, 24576), (8, 8200)], T, n, rank, dt, seed=T + rank, ranks=ranks, y0="in place", pad=8)
+    if T > 2:
+        c.ids[2] = -1
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+def test_broken_adapters_among_few_tokens_over_long_rows(dt):
+    """As above, in the form of two launches for up to 16 tokens."""
+    T, n, rank = 9, 4, 16
+    c = Case([(130, 16384), (64, 20000)], T, n, rank, dt, seed=20)
+    c.ids[:n] = torch.arange(n, dtype=torch.int32)
+    for m in c.mods:
+        m["b"][1, ::3, 0], m["b"][1, 1::3, rank - 1], m["a"][2, 1, 5] = float("nan"), float("inf"), float("inf")
+    c.run()
+    whole = (c.ids != 1) & (c.ids != 2)
+    for m in c.mods:
+        y, mag = su.lora64(m["x"], m["a"], m["b"], c.ids.tolist(), None, c.scales.tolist(), m["src"])
+        bound = su.U32 * (8 + 2 * math.sqrt(m["K"]) + 2 * math.sqrt(rank)) * mag
+        assert ((m["y"].double() - y).abs() <= bound)[whole].all()
+        assert torch.isinf(m["y"][c.ids == 1][:, 1::3]).all()
+
+
+@pytest.mark.parametrize("T,n,rank", [(1, 1, 64), (3, 2, 9), (6, 2, 1)])
+def test_one_launch_and_two_agree(T, n, rank):
+    """The same projection alone (one launch) and beside one of long rows (two): both within the bound, skipped and
+    used tokens in turn."""
+    for shapes in ([(300, 512)], [(300, 512), (16, 1 << 18)]):
+        c = Case(shapes, T, n, rank, torch.bfloat16, seed=30)
+        c.ids[1::2] = -1
+        c.run()
+        c.check()
