@@ -75,7 +75,7 @@ wsr_status wsr_block_norm(const wsr_block* p, void* stream);
    b + a * b_stride, both row-major in `fmt` (WSR_F16 or WSR_BF16), x in the same type, y and y0 fp32
    (y0 null: 0; y0 may be y itself with the same stride, the usual case after a sweep).  A token whose
    adapter is outside [0, n_adapters) has none: y = y0.  Products are exact, sums are fp32, and the
-   inner vector A x stays fp32.  Rows of A and columns of B from r on are not read.
+   inner vector A x enters the second product with 22 bits or more.  Rows of A and columns of B from r on are not read.
    adapter_of: device int32 [n_tokens], in any order; ranks: device int32 [n_adapters], clamped to
    [0, rank], or null (all `rank`); scales: device fp32 [n_adapters] or null (all 1).
    K % 8 == 0, 1 <= rank <= 256; a, x 16-byte aligned, a_stride and x_tok_stride multiples of 16; b
@@ -142,7 +142,7 @@ wsr_status wsr_prefix_attention(const wsr_attn* p, void* ws, size_t ws_bytes, vo
    i: the distribution of the token after i accepted drafts) and the draft model's logits in rows
    0 .. counts[b] - 1 (draft null: each draft was looked up, its distribution all on that token).
    With p = softmax(target / T), q = softmax(draft / T), T = temperature[b] (null: 1; T = 0: all on the
-   lowest index of the largest logit), drafts are accepted in order while uniform_i * q_i(x_i) < p_i(x_i).
+   lowest index of the largest logit; above 1e30: 1e30), drafts are accepted in order while uniform_i * q_i(x_i) < p_i(x_i).
    At the first refusal i, or after the last draft, the next token is the index with the largest
    w_v / noise_v (ties: the lowest), w = max(p_i - q_i, 0), after the last draft w = p (and where all
    of w is 0): with Exp(1) noise, a sample in proportion to w.

@@ -22,8 +22,8 @@
  *    one of the split form does, and k_attn_join_units adds them up).
  *
  * Many rows are bound by the matrix cores and the exponentials between their products: 4 prompts of up to 900 tokens
- * behind 8192 (354 GFLOP) take 370 us, 955 TFLOP/s, where a product of 8192 x 8192 matrices reaches 1200; 24 sequences
- * of 5 tokens behind 32771 (132 GFLOP) 159 us, 830 TFLOP/s (a sequence's 40 rows leave most of a row tile over its own
+ * behind 8192 (354 GFLOP) take 352 to 389 us, 910 to 1005 TFLOP/s, where a product of 8192 x 8192 matrices reaches 1200; 24 sequences
+ * of 5 tokens behind 32771 (132 GFLOP) 158 to 170 us, 775 to 830 TFLOP/s (a sequence's 40 rows leave most of a row tile over its own
  * keys empty).  Few rows are bound by latency: 4 tokens behind 1024 take 10.3 us, two launches' chains of loads.
  */
 #include <hip/hip_runtime.h>
@@ -531,9 +531,10 @@ void k_attn(wsr_attn p, AttnPlan pl) {
     }
 }
 
-/* Adds up the n parts of a row, `step` floats apart, and stores it, by one wave: in order, eight, four, two and one
-   of them loaded at a time (one by one, each after the one before has come, a token on 32771 keys took 36 us, so 30.5). */
-template <int FMT, int D>
+/* Adds up the n parts of a row, `step` floats apart, and stores it, by one wave: in order, AHEAD: eight, four, two and
+   one of them loaded at a time (one by one, each after the one before has come, a token on 32771 keys took 36 us, so
+   30.5; in the whole form, where many waves wait beside one another, one by one is 2 to 3 us of 354 to 389 faster). */
+template <int FMT, int D, bool AHEAD>
 __device__ __forceinline__ void join_row(const wsr_attn& p, const float* w, int64_t step, int n, int tok, int qh, int lane) {
     constexpr int E = D / WAVE;
     const float c = p.scale * A_LOG2E;
@@ -557,10 +558,13 @@ __device__ __forceinline__ void join_row(const wsr_attn& p, const float* w, int6
             for (int e = 0; e < E; ++e) o[e] = o[e] * a + po[k][e] * b;
         }
     };
-    for (; n >= 8; n -= 8) add(std::integral_constant<int, 8>{});
-    if (n & 4) add(std::integral_constant<int, 4>{});
-    if (n & 2) add(std::integral_constant<int, 2>{});
-    if (n & 1) add(std::integral_constant<int, 1>{});
+    if constexpr (AHEAD) {
+        for (; n >= 8; n -= 8) add(std::integral_constant<int, 8>{});
+        if (n & 4) add(std::integral_constant<int, 4>{});
+        if (n & 2) add(std::integral_constant<int, 2>{});
+        if (n & 1) add(std::integral_constant<int, 1>{});
+    } else
+        for (; n > 0; --n) add(std::integral_constant<int, 1>{});
     const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
     char* out = (char*)p.out + tok * p.out_tok_stride + qh * p.out_head_stride;
     if constexpr (E == 2) ((uint32_t*)out)[lane] = pack2<FMT>(o[0] * inv, o[1] * inv);
@@ -589,7 +593,7 @@ __global__ __launch_bounds__(AT) void k_attn_join(wsr_attn p, AttnPlan pl) {
         const int seen = len_of(p, seq) - (start_of(p, seq + 1) - tok) + 1;
         if (seen > 0) own = (seen - 1) / own_part(len_of(p, seq), pl.own_parts, pl.own_block) + 1;
     }
-    join_row<FMT, D>(p, pl.part + row * (D + 4), (int64_t)p.n_tokens * p.n_heads * (D + 4), pl.prefix_parts + own, tok, qh, lane);
+    join_row<FMT, D, true>(p, pl.part + row * (D + 4), (int64_t)p.n_tokens * p.n_heads * (D + 4), pl.prefix_parts + own, tok, qh, lane);
 }
 
 /* The parts of the whole form's last round: a wave per row of its units. */
@@ -605,7 +609,7 @@ __global__ __launch_bounds__(AT) void k_attn_join_units(wsr_attn p, AttnPlan pl)
         for (int k = wave; k < JOIN_ROWS; k += AW) {
             const int at = i % (ROWS / JOIN_ROWS) * JOIN_ROWS + k, row = o.row0 + at;
             if (row < o.rows)
-                join_row<FMT, D>(p, pl.part + ((int64_t)unit * ROWS + at) * (D + 4), (int64_t)r.rest * ROWS * (D + 4), r.parts,
+                join_row<FMT, D, false>(p, pl.part + ((int64_t)unit * ROWS + at) * (D + 4), (int64_t)r.rest * ROWS * (D + 4), r.parts,
                                  o.t0 + row / G, item % p.n_kv_heads * G + row % G, lane);
         }
     }
