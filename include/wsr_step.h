@@ -76,6 +76,7 @@ wsr_status wsr_block_norm(const wsr_block* p, void* stream);
    (y0 null: 0; y0 may be y itself with the same stride, the usual case after a sweep).  A token whose
    adapter is outside [0, n_adapters) has none: y = y0.  Products are exact, sums are fp32, and the
    inner vector A x enters the second product with 22 bits or more.  Rows of A and columns of B from r on are not read.
+   A projection with M = 0 does nothing and may have null pointers; with K = 0, a and x may be null.
    adapter_of: device int32 [n_tokens], in any order; ranks: device int32 [n_adapters], clamped to
    [0, rank], or null (all `rank`); scales: device fp32 [n_adapters] or null (all 1).
    K % 8 == 0, 1 <= rank <= 256; a, x 16-byte aligned, a_stride and x_tok_stride multiples of 16; b

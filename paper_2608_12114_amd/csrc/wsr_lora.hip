@@ -729,14 +729,32 @@ static int tiles_of(int32_t n_tokens) { return (n_tokens + TILE - 1) / TILE; }
 
 static int64_t blocks_of(const wsr_lora& m) { return std::max<int64_t>(1, (m.K + BLOCK_K - 1) / BLOCK_K); }
 
+/* A run: the next projections of a call that one pair of launches takes, of one type and at most a table's length.  Those
+   without rows (M = 0), whose pointers may be null, are in no run: no launch and no workspace knows of them. */
+constexpr int TABLE_MAX = 224;
+struct Run {
+    const wsr_lora* mod[TABLE_MAX];
+    int32_t n = 0;
+};
+/* Fills the run from projection i on; the projection that the next begins with. */
+static int32_t take_run(const wsr_lora* mods, int32_t i, int32_t n, Run& run) {
+    run.n = 0;
+    for (; i < n; ++i) {
+        if (mods[i].M == 0) continue;
+        if (run.n == TABLE_MAX || (run.n && mods[i].fmt != run.mod[0]->fmt)) break;
+        run.mod[run.n++] = &mods[i];
+    }
+    return i;
+}
+
 /* Blocks of K of a shrink workgroup's span at least: spans that give every workgroup the chip holds (two per CU) an
    equal share, of two blocks or more; for many tokens so long that a token's parts, which the second launch adds
    up once per workgroup and projection, stay within 2 KiB. */
-static int least_span(const wsr_lora* mods, int32_t n, int32_t n_tokens) {
+static int least_span(const Run& run, int32_t n_tokens) {
     int64_t all = 0, least = 2;
-    for (int32_t i = 0; i < n; ++i) {
-        all += blocks_of(mods[i]);
-        if (n_tokens > TILE) least = std::max(least, blocks_of(mods[i]) / std::max(1, 512 / mods[i].rank));
+    for (int32_t i = 0; i < run.n; ++i) {
+        all += blocks_of(*run.mod[i]);
+        if (n_tokens > TILE) least = std::max(least, blocks_of(*run.mod[i]) / std::max(1, 512 / run.mod[i]->rank));
     }
     const int64_t held = std::max<int64_t>(1, SHRINK_HELD / tiles_of(n_tokens));
     return (int)std::min<int64_t>(1 << 24, std::max(least, (all + held - 1) / held));
@@ -744,23 +762,15 @@ static int least_span(const wsr_lora* mods, int32_t n, int32_t n_tokens) {
 
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 static size_t order_bytes(int32_t n_tokens) { return n_tokens <= TILE ? 0 : up256(4 * (size_t)n_tokens); }
-constexpr int TABLE_MAX = 224;
 constexpr int64_t SMALL_BYTES = 512 << 10, SMALL_UNITS = 512, SMALL_TOKENS = 3;
-
-/* Runs of projections that one pair of launches takes: of one type, at most a table's length. */
-static int32_t run_of(const wsr_lora* mods, int32_t n) {
-    int32_t i = 1;
-    while (i < n && i < TABLE_MAX && mods[i].fmt == mods[0].fmt) ++i;
-    return i;
-}
 
 /* Places a run's projections: blocks, parts and partial inner vectors; the bytes of the latter, enough for spans of
    `least` blocks or more. */
-static size_t place(const wsr_lora* mods, int32_t n, int32_t n_tokens, int least, int span, LoraMod* out, char* ws) {
+static size_t place(const Run& run, int32_t n_tokens, int least, int span, LoraMod* out, char* ws) {
     int64_t block = 0;
     size_t bytes = 0;
-    for (int32_t i = 0; i < n; ++i) {
-        const wsr_lora& m = mods[i];
+    for (int32_t i = 0; i < run.n; ++i) {
+        const wsr_lora& m = *run.mod[i];
         const int64_t count = blocks_of(m), last = block + count - 1;
         const int pitch = (m.rank + 7) / 8 * 8;
         if (out)
@@ -775,11 +785,10 @@ static size_t place(const wsr_lora* mods, int32_t n, int32_t n_tokens, int least
 
 size_t lora_workspace(const wsr_lora* mods, int32_t n, int32_t n_tokens) {
     size_t most = 256;                         /* the runs follow one another and share it */
-    for (int32_t i = 0; i < n;) {
-        const int32_t k = run_of(mods + i, n - i);
-        const int least = least_span(mods + i, k, n_tokens);
-        most = std::max(most, place(mods + i, k, n_tokens, least, least, nullptr, nullptr));
-        i += k;
+    Run run;
+    for (int32_t i = 0; (i = take_run(mods, i, n, run)), run.n;) {
+        const int least = least_span(run, n_tokens);
+        most = std::max(most, place(run, n_tokens, least, least, nullptr, nullptr));
     }
     return order_bytes(n_tokens) + most;
 }
@@ -864,6 +873,9 @@ static hipError_t launch_table(const LoraMod* mods, int n, int fmt, int64_t bloc
 
 hipError_t launch_lora(const wsr_lora* mods, int32_t n, int32_t n_tokens, const int32_t* adapter_of, int32_t n_adapters,
                        const int32_t* ranks, const float* scales, void* ws, hipStream_t s) {
+    Run run;
+    int32_t next = take_run(mods, 0, n, run);
+    if (run.n == 0) return hipSuccess;         /* no outputs */
     char* at = static_cast<char*>(ws);
     LoraCall c{};
     c.adapter_of = adapter_of, c.ranks = ranks, c.scales = scales, c.n_tokens = n_tokens, c.n_adapters = n_adapters;
@@ -877,12 +889,12 @@ hipError_t launch_lora(const wsr_lora* mods, int32_t n, int32_t n_tokens, const 
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    LoraMod run[TABLE_MAX];
-    for (int32_t i = 0; i < n;) {
-        const int32_t k = run_of(mods + i, n - i);
+    LoraMod placed[TABLE_MAX];
+    for (; run.n; next = take_run(mods, next, n, run)) {
+        const int fmt = run.mod[0]->fmt;
         int64_t blocks = 0;
         int rank = 0;
-        for (int32_t j = i; j < i + k; ++j) blocks += blocks_of(mods[j]), rank = std::max(rank, mods[j].rank);
+        for (int32_t j = 0; j < run.n; ++j) blocks += blocks_of(*run.mod[j]), rank = std::max(rank, run.mod[j]->rank);
         if (blocks > INT32_MAX) return hipErrorInvalidValue;
         /* chunks that a tile can have, and rounds of four 16-row tiles, two chunks each; one such tile is
            enough for a single adapter of 16 ranks (7.4 us with four, so 6.0) */
@@ -892,22 +904,21 @@ hipError_t launch_lora(const wsr_lora* mods, int32_t n, int32_t n_tokens, const 
         /* a round's loads and sums pay from about eight blocks on: where the chip's share is less, several
            workgroups take a longer span and its rounds in turn (`slots`), and where it is more than the call has,
            the rounds are spread over what is left */
-        const int least = least_span(mods + i, k, n_tokens);
+        const int least = least_span(run, n_tokens);
         c.slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, 8 / least));
         /* outputs larger than the chip's second-level caches are gone from them before they are read again: loaded and
            stored past them (16 tokens over the 8B model 277 us, so 258; 2055 prompt tokens 160 and 154) */
         int64_t rows = 0;
-        for (int32_t j = i; j < i + k; ++j) rows += mods[j].M;
+        for (int32_t j = 0; j < run.n; ++j) rows += run.mod[j]->M;
         c.stream = rows * n_tokens * 4 >= 32 << 20;
         const int64_t held = std::max<int64_t>(1, SHRINK_HELD / c.tiles);
         c.span = (int32_t)std::max<int64_t>(least, std::min<int64_t>(8, (blocks * c.slots + held - 1) / held));
         const int64_t spans = (blocks + c.span - 1) / c.span;
         c.slots = (int32_t)std::max<int64_t>(1, std::min<int64_t>(rounds, held / spans));
-        place(mods + i, k, n_tokens, least, c.span, run, at);
-        const hipError_t e = k <= 8 ? launch_table<8>(run, k, mods[i].fmt, blocks, c, one, s)
-                                    : launch_table<TABLE_MAX>(run, k, mods[i].fmt, blocks, c, one, s);
+        place(run, n_tokens, least, c.span, placed, at);
+        const hipError_t e = run.n <= 8 ? launch_table<8>(placed, run.n, fmt, blocks, c, one, s)
+                                    : launch_table<TABLE_MAX>(placed, run.n, fmt, blocks, c, one, s);
         if (e != hipSuccess) return e;
-        i += k;
     }
     return hipSuccess;
 }
