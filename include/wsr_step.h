@@ -114,11 +114,11 @@ wsr_status wsr_lora_sweep(const wsr_lora* mods, int32_t n, int32_t n_tokens, con
    Keys past lens[b] are never read into a result (they may hold anything).  Rows of q that belong to no
    sequence (before starts[0], from starts[n_seqs] on) leave unspecified values in out and lse.
    starts: device int32 [n_seqs + 1], not decreasing, starts[n_seqs] <= n_tokens; lens: device int32
-   [n_seqs], clamped to [0, max_len].  prefix_len and max_len at
-   most 2^30, n_tokens and n_seqs at most 2^20, n_heads at most 4096.  head_dim 64 or 128; every pointer 16-byte aligned and every
-   stride a multiple of 16 (of 4 for lse); tok strides of keys at most 16 MiB; lse (n_tokens, n_heads)
-   or null.  k_prefix and v_prefix (k and v) have the same strides.  ws: wsr_attn_workspace_bytes(),
-   256-byte aligned. */
+   [n_seqs], clamped to [0, max_len].  prefix_len and max_len at most 2^30, together at most 2^31 - 4096;
+   n_tokens and n_seqs at most 2^20, n_heads at most 4096.  head_dim 64 or 128; every pointer 16-byte
+   aligned and every stride a multiple of 16 (of 4 for lse); tok strides of keys at most 16 MiB; lse
+   (n_tokens, n_heads) or null.  k_prefix and v_prefix (k and v) have the same strides.  ws:
+   wsr_attn_workspace_bytes(), 256-byte aligned. */
 typedef struct wsr_attn {
     int32_t fmt, n_heads, n_kv_heads, head_dim, n_seqs, n_tokens;
     float scale;

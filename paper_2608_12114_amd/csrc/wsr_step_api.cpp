@@ -165,6 +165,8 @@ static wsr_status check_attn(const wsr_attn& p, const char* who) {
         return fail(WSR_E_ARG, "%s: negative size", who);
     if (p.n_tokens > 1 << 20 || p.n_seqs > 1 << 20 || p.prefix_len > 1 << 30 || p.max_len > 1 << 30)
         return fail(WSR_E_SIZE, "%s: too many tokens, sequences or keys", who);
+    /* the whole form counts a row's keys, rounded up to whole parts and blocks, in 32 bits */
+    if (p.prefix_len + p.max_len > INT32_MAX - 4095) return fail(WSR_E_SIZE, "%s: more than 2^31 - 4096 keys of a row", who);
     if ((int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads) > 1 << 30) return fail(WSR_E_SIZE, "%s: more than 2^30 rows of a key head", who);
     if (!(p.scale > 0.f) || !std::isfinite(p.scale)) return fail(WSR_E_ARG, "%s: scale must be positive and finite", who);
     if (!p.starts && p.n_tokens != p.n_seqs) return fail(WSR_E_ARG, "%s: without starts each sequence has one token", who);
