@@ -108,8 +108,8 @@ wsr_status wsr_lora_sweep(const wsr_lora* mods, int32_t n, int32_t n_tokens, con
    row b); they are its last n_b of lens[b] own keys.  Query i of sequence b sees all prefix_len keys
    of the prefix and its own keys j < lens[b] - n_b + i + 1:
      out = sum_k softmax_k(scale q . key_k) value_k,  lse = log sum_k exp(scale q . key_k).
-   A row that sees no key gets out = 0 and lse = -inf.  Query head h reads key head
-   h / (n_heads / n_kv_heads).  Types `fmt` (WSR_F16 or WSR_BF16); scores, softmax statistics and sums
+   A row that sees no key gets out = 0 and lse = -inf, one with a NaN among its scores NaN in both.  Query
+   head h reads key head h / (n_heads / n_kv_heads).  Types `fmt` (WSR_F16 or WSR_BF16); scores, softmax statistics and sums
    are fp32, probabilities are rounded to `fmt` for the product with the values, out once to `fmt`.
    Keys past lens[b] are never read into a result (they may hold anything).  Rows of q that belong to no
    sequence (before starts[0], from starts[n_seqs] on) leave unspecified values in out and lse.

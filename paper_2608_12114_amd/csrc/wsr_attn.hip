@@ -109,6 +109,10 @@ __device__ __forceinline__ int count_tiles(const wsr_attn& p, int G, int rows) {
     return __builtin_amdgcn_readfirstlane(n);
 }
 
+/* log of a row's sum l against its maximum m: -inf where it saw no key, and NaN, like its outputs, where a score was NaN,
+   which leaves no trace in the maximum. */
+__device__ __forceinline__ float lse_of(float m, float l, float scale) { return l == 0.f ? A_NEG_INF : m * scale + logf(l); }
+
 /* Keys of a part of a sequence's `own` keys (split form): of at most `parts` equal ones, whole blocks, LEAST or more
    where joining one costs less than the keys.  Taken from the length and not from the room that the cache has. */
 constexpr int LEAST = 256;
@@ -516,7 +520,7 @@ void k_attn(wsr_attn p, AttnPlan pl) {
                 *(u32x2*)(out + (32 * i + 8 * j + 4 * h) * 2) =
                     u32x2{pack2<FMT>(a.o[i][4 * j] * inv, a.o[i][4 * j + 1] * inv),
                           pack2<FMT>(a.o[i][4 * j + 2] * inv, a.o[i][4 * j + 3] * inv)};
-        if (p.lse && h == 0) p.lse[(int64_t)tok * p.n_heads + qh] = a.m == A_NEG_INF ? a.m : a.m * p.scale + logf(a.l);
+        if (p.lse && h == 0) p.lse[(int64_t)tok * p.n_heads + qh] = lse_of(a.m, a.l, p.scale);
     } else {
         const int64_t slot = WHOLE ? (int64_t)(blockIdx.x % HELD) * ROWS + row - row0  /* full is a multiple of HELD */
                                    : ((int64_t)(prefix ? part : pl.prefix_parts + part) * p.n_tokens + tok) * p.n_heads + qh;
@@ -569,7 +573,7 @@ __device__ __forceinline__ void join_row(const wsr_attn& p, const float* w, int6
     char* out = (char*)p.out + tok * p.out_tok_stride + qh * p.out_head_stride;
     if constexpr (E == 2) ((uint32_t*)out)[lane] = pack2<FMT>(o[0] * inv, o[1] * inv);
     else ((uint16_t*)out)[lane] = (uint16_t)pack2<FMT>(o[0] * inv, 0.f);
-    if (p.lse && lane == 0) p.lse[(int64_t)tok * p.n_heads + qh] = m == A_NEG_INF ? m : m * p.scale + logf(l);
+    if (p.lse && lane == 0) p.lse[(int64_t)tok * p.n_heads + qh] = lse_of(m, l, p.scale);
 }
 
 /* One wave per (token, head): the parts that were written, in order. */
