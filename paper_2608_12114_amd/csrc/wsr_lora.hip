@@ -389,17 +389,19 @@ __device__ __forceinline__ void make_inner(const LoraMod& d, const LoraCall& c, 
     for (int token = threadIdx.x / 16; token < COLS; token += LT / 16) {
         f4_t s = load(token, w0 + 4 * q);
         if constexpr (FMT == WSR_F16) {
+            /* the largest finite entry: beside an infinity the others are still to keep within f16 */
             float top = 0.f;
-            if (d.rank <= WINDOW) top = fmaxf(fmaxf(fabsf(s[0]), fabsf(s[1])), fmaxf(fabsf(s[2]), fabsf(s[3])));
+            auto larger = [&](f4_t o) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = fabsf(o[e]) < __builtin_inff() ? fmaxf(top, fabsf(o[e])) : top;
+            };
+            if (d.rank <= WINDOW) larger(s);
             else
-                for (int w = 0; w < d.rank; w += WINDOW) {
-                    const f4_t o = load(token, w + 4 * q);
-                    top = fmaxf(top, fmaxf(fmaxf(fabsf(o[0]), fabsf(o[1])), fmaxf(fabsf(o[2]), fabsf(o[3]))));
-                }
+                for (int w = 0; w < d.rank; w += WINDOW) larger(load(token, w + 4 * q));
 #pragma unroll
             for (int k = 1; k < 16; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
             /* 2^9 <= scaled top < 2^10, the exponent kept where both powers of two are normal */
-            const int e = top > 0.f && top < __builtin_inff() ? min(max(10 - __builtin_amdgcn_frexp_expf(top), -110), 110) : 0;
+            const int e = top > 0.f ? min(max(10 - __builtin_amdgcn_frexp_expf(top), -110), 110) : 0;
             s *= __builtin_amdgcn_ldexpf(1.f, e);
             if (q == 0) in.undo[token] = __builtin_amdgcn_ldexpf(1.f, -e);
         }
