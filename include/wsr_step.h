@@ -75,7 +75,9 @@ wsr_status wsr_block_norm(const wsr_block* p, void* stream);
    b + a * b_stride, both row-major in `fmt` (WSR_F16 or WSR_BF16), x in the same type, y and y0 fp32
    (y0 null: 0; y0 may be y itself with the same stride, the usual case after a sweep).  A token whose
    adapter is outside [0, n_adapters) has none: y = y0.  Products are exact, sums are fp32, and the
-   inner vector A x enters the second product with 22 bits or more.  Rows of A and columns of B from r on are not read.
+   inner vector A x enters the second product with 24 bits (WSR_BF16), or with 22 (WSR_F16: entries down to
+   2^-28 of the token's largest; smaller ones within 2^-50 of it).  Rows of A and columns of B from r on are
+   not read.
    A projection with M = 0 does nothing and may have null pointers; with K = 0, a and x may be null.
    adapter_of: device int32 [n_tokens], in any order; ranks: device int32 [n_adapters], clamped to
    [0, rank], or null (all `rank`); scales: device fp32 [n_adapters] or null (all 1).

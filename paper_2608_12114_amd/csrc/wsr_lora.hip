@@ -17,7 +17,8 @@
  *                   the products, so that a token's sums do not depend on the tile that the order, which is free
  *                   inside an adapter, put it in.  The inner vectors are fp32 (24 bits): they enter as the sum of
  *                   three bf16 terms (24 bits) or of two f16 terms (22 bits, each token's vector scaled by a
- *                   power of two so that its largest entry is near 2^10), products with B exact, sums fp32.
+ *                   power of two so that its largest entry is near 2^15, the second term by 2^11 more, which
+ *                   keeps entries 2^-28 of the largest whole), products with B exact, sums fp32.
  *                   Rounding them to one 16-bit term would leave errors of 2^-9 in the fp32 outputs.
  *
  * Decode is bound by reading the adapters (2 (K + M) rank bytes each): 16 tokens of 14 adapters of 16 ranks over
@@ -355,6 +356,19 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 w) {
 
 template <int FMT>
 constexpr int terms() { return FMT == WSR_BF16 ? 3 : 2; }
+/* What a term after the first is multiplied by.  An f16 residual would fall below the type's smallest steps where an entry
+   is far below the token's largest: it gets a power of two of its own, which accumulate() takes off the product. */
+template <int FMT>
+constexpr float lift() { return FMT == WSR_BF16 ? 1.f : 2048.f; }
+/* c + w v_k, term k of the inner vectors. */
+template <int FMT>
+__device__ __forceinline__ f4_t accumulate(u32x4 w, u32x4 v, f4_t c, int k) {
+    if (FMT == WSR_BF16 || k == 0) return mma_16x16x32<FMT>(w, v, c);
+    const f4_t p = mma_16x16x32<FMT>(w, v, f4_t{0, 0, 0, 0});
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = fmaf(p[e], 1.f / lift<FMT>(), c[e]);
+    return c;
+}
 
 /* The inner vectors of a window in LDS as 16-bit terms, and the power of two that undoes each token's
    scaling.  A pitch of 16 bytes past a multiple of 128 keeps the 16 tokens' reads on different banks. */
@@ -400,8 +414,8 @@ __device__ __forceinline__ void make_inner(const LoraMod& d, const LoraCall& c, 
                 for (int w = 0; w < d.rank; w += WINDOW) larger(load(token, w + 4 * q));
 #pragma unroll
             for (int k = 1; k < 16; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
-            /* 2^9 <= scaled top < 2^10, the exponent kept where both powers of two are normal */
-            const int e = top > 0.f ? min(max(10 - __builtin_amdgcn_frexp_expf(top), -110), 110) : 0;
+            /* 2^14 <= scaled top < 2^15, the exponent kept where both powers of two are normal */
+            const int e = top > 0.f ? min(max(15 - __builtin_amdgcn_frexp_expf(top), -126), 126) : 0;
             s *= __builtin_amdgcn_ldexpf(1.f, e);
             if (q == 0) in.undo[token] = __builtin_amdgcn_ldexpf(1.f, -e);
         }
@@ -413,7 +427,7 @@ __device__ __forceinline__ void make_inner(const LoraMod& d, const LoraCall& c, 
             for (int e = 0; e < 2; ++e) {
                 w[e] = pack2<FMT>(s[2 * e], s[2 * e + 1]);
                 const float a = s[2 * e] - (float)(H)s[2 * e], b = s[2 * e + 1] - (float)(H)s[2 * e + 1];
-                s[2 * e] = a == a ? a : 0.f, s[2 * e + 1] = b == b ? b : 0.f;   /* inf - inf */
+                s[2 * e] = a == a ? a * lift<FMT>() : 0.f, s[2 * e + 1] = b == b ? b * lift<FMT>() : 0.f;   /* inf - inf */
             }
             *(u32x2*)(in.v + token * I::PITCH + k * WINDOW + 4 * q) = w;
         }
@@ -531,7 +545,7 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(expand_waves
 #pragma unroll
                             for (int k = 0; k < NTERM; ++k)
 #pragma unroll
-                                for (int i = 0; i < RW; ++i) acc[i][j] = mma_16x16x32<FMT>(b[u][i], v[k], acc[i][j]);
+                                for (int i = 0; i < RW; ++i) acc[i][j] = accumulate<FMT>(b[u][i], v[k], acc[i][j], k);
                         } else {
 #pragma unroll 1
                             for (int o = 0; o < 4; ++o) {
@@ -545,7 +559,7 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(expand_waves
                                     asm volatile("" : "+v"(w));          /* or the next line's registers are held all along */
 #pragma unroll
                                     for (int k = 0; k < NTERM; ++k) {
-                                        s = mma_16x16x32<FMT>(w, v[k], s);
+                                        s = accumulate<FMT>(w, v[k], s, k);
                                         if (k == 0) w = finite_only<FMT>(w);   /* later terms may differ in sign */
                                     }
 #pragma unroll
