@@ -238,12 +238,21 @@ def wsr_decode_sweep_mma(mats, n_tokens: int, ws, ws_bytes: int, stream=None) ->
     _check(_L.wsr_decode_sweep_mma(mats, _n(mats), n_tokens, _ptr(ws), ws_bytes, _stream(stream)))
 
 
+_STEP_NAMES = frozenset((
+    "WSR_NORM_RMS", "WSR_NORM_LAYER", "WSR_BLOCK_POST", "wsr_block", "wsr_lora", "wsr_attn", "wsr_verify", "make_block", "make_loras",
+    "make_attn", "make_verify", "step_lib", "wsr_step_last_error", "wsr_block_norm", "wsr_lora_workspace_bytes", "wsr_lora_sweep",
+    "wsr_attn_workspace_bytes", "wsr_prefix_attention", "wsr_verify_workspace_bytes", "wsr_verify_drafts"))
+
+
 def __getattr__(name):
     """The entry points of include/wsr_step.h (wsr_block_norm, wsr_lora_sweep, wsr_prefix_attention,
-    wsr_verify_drafts and what belongs to them), from the binding of libwsr_step.so: loaded on first use."""
-    if name.startswith("_"):
-        raise AttributeError(name)
-    from . import wsr_step
-    value = getattr(wsr_step, name)
-    globals()[name] = value
+    wsr_verify_drafts and what belongs to them), from the binding of libwsr_step.so: loaded on first use.
+    Any other name, and these where that library is not built, is an AttributeError."""
+    if name not in _STEP_NAMES:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    try:
+        from . import wsr_step
+    except ImportError as e:
+        raise AttributeError(f"{name}: {e}") from e
+    value = globals()[name] = getattr(wsr_step, name)
     return value
