@@ -41,7 +41,7 @@ const char* wsr_step_last_error(void);
    where their pointers are null.  h' is stored to h_out (if not null) in fp32, x is rounded once to
    `fmt` (WSR_F16 or WSR_BF16), the type of w, b and gate too.  All arithmetic is fp32; an infinity or
    NaN in a token's inputs reaches that token's outputs only.
-   d % 8 == 0, d <= 32768; rows and vectors 16-byte aligned, token strides multiples of 16.  gate:
+   d % 8 == 0, d <= 32768, n_tokens < 2^31; rows and vectors 16-byte aligned, token strides multiples of 16.  gate:
    one vector for all tokens (stride 0) or one per token.  h_out may be h itself (same stride);
    outputs otherwise overlap nothing. */
 #define WSR_NORM_RMS 0
@@ -83,7 +83,7 @@ wsr_status wsr_block_norm(const wsr_block* p, void* stream);
    [0, rank], or null (all `rank`); scales: device fp32 [n_adapters] or null (all 1).
    K % 8 == 0, 1 <= rank <= 256; a, x 16-byte aligned, a_stride and x_tok_stride multiples of 16; b
    2-byte aligned; y, y0 4-byte aligned, strides multiples of 4, y_tok_stride >= 4 M for more than one
-   token.  n_tokens <= 2^20 and n_adapters <= 8192.  ws: wsr_lora_workspace_bytes(), 256-byte aligned,
+   token.  n_tokens <= 2^20, n_adapters <= 8192, M < 2^31, K <= 2^28, 2^36 rows in all.  ws: wsr_lora_workspace_bytes(), 256-byte aligned,
    read and written by this call only. */
 typedef struct wsr_lora {
     int32_t fmt, rank;
@@ -117,7 +117,8 @@ wsr_status wsr_lora_sweep(const wsr_lora* mods, int32_t n, int32_t n_tokens, con
    sequence (before starts[0], from starts[n_seqs] on) leave unspecified values in out and lse.
    starts: device int32 [n_seqs + 1], not decreasing, starts[n_seqs] <= n_tokens; lens: device int32
    [n_seqs], clamped to [0, max_len].  prefix_len and max_len at most 2^30, together at most 2^31 - 4096;
-   n_tokens and n_seqs at most 2^20, n_heads at most 4096.  head_dim 64 or 128; every pointer 16-byte
+   n_tokens and n_seqs at most 2^20, n_heads at most 4096, rows of a key head (tokens times its query heads) at
+   most 2^30; calls with n_kv_heads * (n_seqs + those rows / 128) past 2^22 may be refused.  head_dim 64 or 128; every pointer 16-byte
    aligned and every stride a multiple of 16 (of 4 for lse); tok strides of keys at most 16 MiB; lse
    (n_tokens, n_heads) or null.  k_prefix and v_prefix (k and v) have the same strides.  ws:
    wsr_attn_workspace_bytes(), 256-byte aligned. */
@@ -158,7 +159,7 @@ wsr_status wsr_prefix_attention(const wsr_attn* p, void* ws, size_t ws_bytes, vo
    target, draft: fp32, strides multiples of 4, rows 4-byte aligned; tokens: int32 (n_seqs, n_drafts);
    uniform: fp32 (n_seqs, n_drafts) in [0, 1); noise: fp32 (n_seqs, vocab), positive and normal;
    counts, temperature: device [n_seqs], counts clamped to [0, n_drafts].  1 <= vocab <= 2^24,
-   0 <= n_drafts <= 63.  ws: wsr_verify_workspace_bytes(), 256-byte aligned. */
+   0 <= n_drafts <= 63, n_seqs <= 2^16.  ws: wsr_verify_workspace_bytes(), 256-byte aligned. */
 typedef struct wsr_verify {
     int32_t n_seqs, n_drafts;
     int64_t vocab;

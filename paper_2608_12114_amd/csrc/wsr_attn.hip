@@ -576,10 +576,10 @@ __device__ __forceinline__ void join_row(const wsr_attn& p, const float* w, int6
     if (p.lse && lane == 0) p.lse[(int64_t)tok * p.n_heads + qh] = lse_of(m, l, p.scale);
 }
 
-/* One wave per (token, head): the parts that were written, in order. */
+/* One wave per (token, head), from row `first` on: the parts that were written, in order. */
 template <int FMT, int D>
-__global__ __launch_bounds__(AT) void k_attn_join(wsr_attn p, AttnPlan pl) {
-    const int64_t row = (int64_t)blockIdx.x * AW + wsr::wave_in_block();
+__global__ __launch_bounds__(AT) void k_attn_join(wsr_attn p, AttnPlan pl, int64_t first) {
+    const int64_t row = first + (int64_t)blockIdx.x * AW + wsr::wave_in_block();
     const int lane = threadIdx.x % WAVE;
     if (row >= (int64_t)p.n_tokens * p.n_heads) return;
     const int tok = (int)(row / p.n_heads), qh = (int)(row % p.n_heads);
@@ -651,6 +651,13 @@ static AttnPlan attn_plan(const wsr_attn& p) {
     return pl;
 }
 
+/* Workgroups of the first launch. */
+static int64_t attn_blocks(const wsr_attn& p, const AttnPlan& pl) {
+    const int64_t items = pl.whole ? pl.own_tiles : (int64_t)pl.prefix_tiles * pl.prefix_parts + (int64_t)pl.own_tiles * pl.own_parts;
+    return items * p.n_kv_heads + (pl.whole && pl.most_parts > 1 ? HELD : 0);
+}
+bool attn_fits(const wsr_attn& p) { return attn_blocks(p, attn_plan(p)) <= most_blocks(AT); }
+
 size_t attn_workspace(const wsr_attn& p) {
     const AttnPlan pl = attn_plan(p);
     if (pl.whole) return pl.most_parts > 1 ? (size_t)HELD * 128 * (p.head_dim + 4) * 4 : 256;
@@ -659,9 +666,7 @@ size_t attn_workspace(const wsr_attn& p) {
 
 template <int FMT, int D>
 static hipError_t launch_dim(const wsr_attn& p, const AttnPlan& pl, hipStream_t s) {
-    const int64_t items = pl.whole ? pl.own_tiles : (int64_t)pl.prefix_tiles * pl.prefix_parts + (int64_t)pl.own_tiles * pl.own_parts;
-    const int64_t blocks = items * p.n_kv_heads + (pl.whole && pl.most_parts > 1 ? HELD : 0);
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
+    const int64_t blocks = attn_blocks(p, pl);
     const dim3 grid((unsigned)blocks), threads(AT);
     if (blocks > 0) {
         if (pl.whole) hipLaunchKernelGGL((k_attn<FMT, D, 4, true>), grid, threads, 0, s, p, pl);
@@ -678,8 +683,13 @@ static hipError_t launch_dim(const wsr_attn& p, const AttnPlan& pl, hipStream_t 
         return hipGetLastError();
     }
     const int64_t rows = (int64_t)p.n_tokens * p.n_heads;
-    hipLaunchKernelGGL((k_attn_join<FMT, D>), dim3((unsigned)((rows + AW - 1) / AW)), threads, 0, s, p, pl);
-    return hipGetLastError();
+    for (int64_t first = 0; first < rows; first += most_blocks(AT) * AW) {
+        const int64_t n = std::min((rows - first + AW - 1) / AW, most_blocks(AT));
+        hipLaunchKernelGGL((k_attn_join<FMT, D>), dim3((unsigned)n), threads, 0, s, p, pl, first);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_attn(const wsr_attn& p, void* ws, hipStream_t s) {

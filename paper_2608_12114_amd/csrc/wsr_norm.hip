@@ -8,6 +8,9 @@
  */
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "wsr_step_device.h"
 
 namespace wsr_step {
@@ -132,34 +135,39 @@ __global__ __launch_bounds__(WAVES * WAVE) void k_block_norm(wsr_block p) {
    6.14).  A residual stream larger than the chip's second-level caches is gone from them before it is read
    again, so it is stored past them (8193 x 4096 86.8 us, so 84.8; 8193 x 1160 29.4 and 26.1). */
 constexpr int64_t STREAM_FROM = 32 << 20;
-template <int FMT, int KIND>
-static void launch_kind(const wsr_block& p, hipStream_t s) {
+template <int FMT, int KIND, int W, int NC>
+static hipError_t launch_waves(wsr_block p, hipStream_t s) {
     const bool stream = p.n_tokens * p.d * 4 >= STREAM_FROM;
-#define WSR_NORM(W, NC)                                                                                                      \
-    do {                                                                                                                     \
-        const dim3 grid((unsigned)p.n_tokens), threads(W * WAVE);                                                            \
-        if (stream) hipLaunchKernelGGL((k_block_norm<FMT, KIND, W, NC, true>), grid, threads, 0, s, p);                      \
-        else hipLaunchKernelGGL((k_block_norm<FMT, KIND, W, NC, false>), grid, threads, 0, s, p);                            \
-    } while (0)
-    if (p.d <= 512) WSR_NORM(1, 1);
-    else if (p.d <= 2048) WSR_NORM(4, 1);
-    else if (p.d <= 4096) WSR_NORM(8, 1);
-    else if (p.d <= 8192 && p.n_tokens >= 512) WSR_NORM(8, 2);
-    else if (p.d <= 8192) WSR_NORM(16, 1);
-    else if (p.d <= 16384) WSR_NORM(16, 2);
-    else WSR_NORM(16, 4);
-#undef WSR_NORM
+    /* of its rows as many as a launch holds, then the next */
+    auto ahead = [](auto*& at, int64_t bytes) {
+        if (at) at = (std::remove_reference_t<decltype(at)>)((const char*)at + bytes);
+    };
+    for (int64_t left = p.n_tokens, n; left > 0; left -= n) {
+        n = std::min(left, most_blocks(W * WAVE));
+        const dim3 grid((unsigned)n), threads(W * WAVE);
+        if (stream) hipLaunchKernelGGL((k_block_norm<FMT, KIND, W, NC, true>), grid, threads, 0, s, p);
+        else hipLaunchKernelGGL((k_block_norm<FMT, KIND, W, NC, false>), grid, threads, 0, s, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        ahead(p.y, n * p.y_tok_stride), ahead(p.gate, n * p.gate_tok_stride), ahead(p.h, n * p.h_tok_stride);
+        ahead(p.h_out, n * p.h_out_tok_stride), ahead(p.x, n * p.x_tok_stride);
+    }
+    return hipSuccess;
+}
+template <int FMT, int KIND>
+static hipError_t launch_kind(const wsr_block& p, hipStream_t s) {
+    if (p.d <= 512) return launch_waves<FMT, KIND, 1, 1>(p, s);
+    if (p.d <= 2048) return launch_waves<FMT, KIND, 4, 1>(p, s);
+    if (p.d <= 4096) return launch_waves<FMT, KIND, 8, 1>(p, s);
+    if (p.d <= 8192 && p.n_tokens >= 512) return launch_waves<FMT, KIND, 8, 2>(p, s);
+    if (p.d <= 8192) return launch_waves<FMT, KIND, 16, 1>(p, s);
+    if (p.d <= 16384) return launch_waves<FMT, KIND, 16, 2>(p, s);
+    return launch_waves<FMT, KIND, 16, 4>(p, s);
 }
 
 hipError_t launch_block_norm(const wsr_block& p, hipStream_t s) {
-    if (p.fmt == WSR_F16) {
-        if (p.kind == WSR_NORM_RMS) launch_kind<WSR_F16, WSR_NORM_RMS>(p, s);
-        else launch_kind<WSR_F16, WSR_NORM_LAYER>(p, s);
-    } else {
-        if (p.kind == WSR_NORM_RMS) launch_kind<WSR_BF16, WSR_NORM_RMS>(p, s);
-        else launch_kind<WSR_BF16, WSR_NORM_LAYER>(p, s);
-    }
-    return hipGetLastError();
+    if (p.fmt == WSR_F16) return p.kind == WSR_NORM_RMS ? launch_kind<WSR_F16, WSR_NORM_RMS>(p, s) : launch_kind<WSR_F16, WSR_NORM_LAYER>(p, s);
+    return p.kind == WSR_NORM_RMS ? launch_kind<WSR_BF16, WSR_NORM_RMS>(p, s) : launch_kind<WSR_BF16, WSR_NORM_LAYER>(p, s);
 }
 
 }  // namespace wsr_step

@@ -132,6 +132,9 @@ static wsr_status check_loras(const wsr_lora* mods, int32_t n, int32_t n_tokens,
         if (m.y0 == m.y && n_tokens > 1 && m.y0_tok_stride != m.y_tok_stride)
             return fail(WSR_E_ARG, "%s: y0 in place of y needs the same stride", at);
     }
+    int64_t rows = 0;
+    for (int32_t i = 0; i < n; ++i) rows += mods[i].M;
+    if (rows > (int64_t)1 << 36) return fail(WSR_E_SIZE, "%s: more than 2^36 rows", who);
     return WSR_OK;
 }
 
@@ -171,6 +174,7 @@ static wsr_status check_attn(const wsr_attn& p, const char* who) {
     if (!(p.scale > 0.f) || !std::isfinite(p.scale)) return fail(WSR_E_ARG, "%s: scale must be positive and finite", who);
     if (!p.starts && p.n_tokens != p.n_seqs) return fail(WSR_E_ARG, "%s: without starts each sequence has one token", who);
     if (p.n_seqs == 0 && p.n_tokens > 0) return fail(WSR_E_ARG, "%s: tokens of no sequence", who);
+    if (!wsr_step::attn_fits(p)) return fail(WSR_E_SIZE, "%s: too many sequences and key heads for one launch", who);
     return WSR_OK;
 }
 

@@ -325,9 +325,8 @@ static hipError_t launch_two(const wsr_verify& p, const VerifyPlan& v, char* ws,
     Stat* stats = reinterpret_cast<Stat*>(ws);
     Words* best = reinterpret_cast<Words*>(ws + v.best_at);
     uint32_t* done = reinterpret_cast<uint32_t*>(ws + v.done_at);
-    const int64_t blocks = (int64_t)p.n_seqs * v.rows * v.chunks;
-    if (blocks > INT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(k_verify_stats<VU>, dim3((unsigned)blocks), dim3(VT), 0, s, p, stats, done, v.rows, v.chunks);
+    hipLaunchKernelGGL(k_verify_stats<VU>, dim3((unsigned)(p.n_seqs * v.rows * v.chunks)), dim3(VT), 0, s, p, stats, done, v.rows,
+                       v.chunks);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_verify_race<VU>, dim3((unsigned)(p.n_seqs * v.chunks)), dim3(VT), 0, s, p, stats, best, done, v.rows,
@@ -337,7 +336,23 @@ static hipError_t launch_two(const wsr_verify& p, const VerifyPlan& v, char* ws,
 
 hipError_t launch_verify(const wsr_verify& p, void* ws, hipStream_t s) {
     const VerifyPlan v = plan_of(p);
-    return v.fine ? launch_two<2>(p, v, static_cast<char*>(ws), s) : launch_two<4>(p, v, static_cast<char*>(ws), s);
+    /* as many sequences as a launch holds the rows and chunks of, then the next, in the same workspace */
+    const int64_t held = most_blocks(VT) / ((int64_t)v.rows * v.chunks);
+    for (int64_t b = 0; b < p.n_seqs; b += held) {
+        wsr_verify q = p;
+        q.n_seqs = (int32_t)std::min<int64_t>(held, p.n_seqs - b);
+        q.target = (const float*)((const char*)p.target + b * p.target_seq_stride);
+        if (p.draft) q.draft = (const float*)((const char*)p.draft + b * p.draft_seq_stride);
+        q.noise = (const float*)((const char*)p.noise + b * p.noise_seq_stride);
+        if (p.n_drafts) q.tokens += b * p.n_drafts, q.uniform += b * p.n_drafts;
+        if (p.counts) q.counts += b;
+        if (p.temperature) q.temperature += b;
+        q.out += b * (p.n_drafts + 1), q.accepted += b;
+        if (p.logp) q.logp += b * (p.n_drafts + 1);
+        const hipError_t e = v.fine ? launch_two<2>(q, v, static_cast<char*>(ws), s) : launch_two<4>(q, v, static_cast<char*>(ws), s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace wsr_step
