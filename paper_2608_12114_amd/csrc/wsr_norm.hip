@@ -4,7 +4,7 @@
  *   v = post(y),  h' = s h + g v,  x = pre(h'):  each row is read once, held in registers through
  *   both norms and written once (14 bytes per element with h' and x), so the kernel is bound by HBM
  *   for prompts (4099 x 8192 layer norms, 537 MB, 97 us, 5.5 TB/s; a copy of 1 GiB reaches 4.8) and by one row's
-   latency (loads, two or four workgroup sums, stores) for few tokens (one of 4096 3.0 us).
+ *   latency (loads, two or four workgroup sums, stores) for few tokens (one of 4096 3.0 us).
  */
 #include <hip/hip_runtime.h>
 
@@ -130,9 +130,9 @@ __global__ __launch_bounds__(WAVES * WAVE) void k_block_norm(wsr_block p) {
     }
 }
 
-/* Few tokens: as many threads as the row has pieces, for the shortest chain.  Many tokens of 4104 to 8192
-   elements: two pieces each (4099 tokens 111.8 us with one, so 107.2; 16 tokens 4.62 and 4.73, 64 tokens 5.70 and
-   6.14).  A residual stream larger than the chip's second-level caches is gone from them before it is read
+/* As many threads as the row has pieces, up to eight waves: with sixteen the sums take longer than the second pieces
+   (rms of 8192 elements, one piece each and two: 1 token 4.8 us, so 4.4; 64 tokens 5.3 and 4.9, 512 13.3 and 12.2;
+   4104 elements, 1 token 4.1 and 3.8; 4099 x 8192 layer norms 88.6 and 86.5).  A residual stream larger than the chip's second-level caches is gone from them before it is read
    again, so it is stored past them (8193 x 4096 86.8 us, so 84.8; 8193 x 1160 29.4 and 26.1). */
 constexpr int64_t STREAM_FROM = 32 << 20;
 template <int FMT, int KIND, int W, int NC>
@@ -159,8 +159,7 @@ static hipError_t launch_kind(const wsr_block& p, hipStream_t s) {
     if (p.d <= 512) return launch_waves<FMT, KIND, 1, 1>(p, s);
     if (p.d <= 2048) return launch_waves<FMT, KIND, 4, 1>(p, s);
     if (p.d <= 4096) return launch_waves<FMT, KIND, 8, 1>(p, s);
-    if (p.d <= 8192 && p.n_tokens >= 512) return launch_waves<FMT, KIND, 8, 2>(p, s);
-    if (p.d <= 8192) return launch_waves<FMT, KIND, 16, 1>(p, s);
+    if (p.d <= 8192) return launch_waves<FMT, KIND, 8, 2>(p, s);
     if (p.d <= 16384) return launch_waves<FMT, KIND, 16, 2>(p, s);
     return launch_waves<FMT, KIND, 16, 4>(p, s);
 }
