@@ -841,9 +841,11 @@ static hipError_t launch_pair(LoraTable<N>& tab, const LoraCall& c, bool one, hi
     else hipLaunchKernelGGL((k_lora_shrink<FMT, TT, 4, N>), grid, dim3(LT), 0, s, tab, c);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    /* units of 64 rows instead of 128 where the latter would leave half of the chip's places empty */
+    /* units of 64 rows instead of 128 where the latter would take less than three eighths of the chip's 1024 places (16
+       tokens of 14 adapters, 64 and 128: 43008 rows 25.3 and 26.1 us, 57344 23.2 and 22.5, 86016 37.3 and 33.1; 4 tokens
+       of 64 ranks, 40960 rows 22.4 and 23.0, 61440 28.0 and 27.4) */
     if constexpr (TT == 1)
-        if (rows / 256 < 512) return launch_expand<FMT, 1, 1, false, N>(tab, c, s);
+        if (rows / 128 < 384) return launch_expand<FMT, 1, 1, false, N>(tab, c, s);
     if (c.stream) return launch_expand<FMT, TT, 2, true, N>(tab, c, s);
     return launch_expand<FMT, TT, 2, false, N>(tab, c, s);
 }
