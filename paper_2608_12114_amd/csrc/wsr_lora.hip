@@ -778,7 +778,7 @@ static int least_span(const Run& run, int32_t n_tokens) {
 
 static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 static size_t order_bytes(int32_t n_tokens) { return n_tokens <= TILE ? 0 : up256(4 * (size_t)n_tokens); }
-constexpr int64_t SMALL_BYTES = 512 << 10, SMALL_UNITS = 512, SMALL_TOKENS = 3;
+constexpr int64_t SMALL_BYTES[] = {448 << 10, 256 << 10, 192 << 10}, SMALL_TOKENS = 3, SMALL_UNITS = 512;
 
 /* Places a run's projections: blocks, parts and partial inner vectors; the bytes of the latter, enough for spans of
    `least` blocks or more. */
@@ -850,14 +850,15 @@ static hipError_t launch_pair(LoraTable<N>& tab, const LoraCall& c, bool one, hi
     return launch_expand<FMT, TT, 2, false, N>(tab, c, s);
 }
 
-/* Whether one launch does: every workgroup reads all of the tokens' rows of A, so they are to be short, the
-   workgroups few and the tokens, which go one after the other, few (1 token over three projections of up to 448 KiB of A, 168 workgroups, 9.1 us, in
-   two launches 12.3; 3 tokens over 384 KiB 13.3 and 12.9, where the host's launch is saved still; 1 MiB 26 and 14). */
+/* Whether one launch does: every workgroup reads all of the tokens' rows of A, so they are to be short, the workgroups few
+   and the tokens, which go one after the other, few.  By the bytes of A that a workgroup reads, one launch and two (us):
+   1 token 128 KiB 6.1 and 10.1, 256 KiB 9.4 and 12.5, 448 KiB 11.2 and 11.7, 512 KiB 13.4 and 13.0; 2 tokens 256 KiB 10.1
+   and 12.2, 290 KiB 20.4 and 15.8; 3 tokens 192 KiB 11.4 and 12.2, 217 KiB 14.9 and 15.2, 240 KiB 13.3 and 10.5. */
 static bool is_small(const LoraMod* mods, int n, int32_t n_tokens) {
     if (n_tokens > SMALL_TOKENS) return false;
     int64_t units = 0;
     for (int i = 0; i < n; ++i) {
-        if (mods[i].rank > SMALL_RANK || n_tokens * mods[i].rank * mods[i].K * 2 > SMALL_BYTES) return false;
+        if (mods[i].rank > SMALL_RANK || n_tokens * mods[i].rank * mods[i].K * 2 > SMALL_BYTES[n_tokens - 1]) return false;
         units += (mods[i].M + LT - 1) / LT;
     }
     return units <= SMALL_UNITS;
