@@ -32,7 +32,6 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "wsr_mma.h"
 #include "wsr_step_device.h"
 
 namespace wsr_step {
@@ -253,7 +252,7 @@ __global__ __launch_bounds__(LT) void k_lora_shrink(LoraTable<N> tab, LoraCall c
 #pragma unroll
                         for (int h = 0; h < 2; ++h)
 #pragma unroll
-                            for (int j = 0; j < TT; ++j) acc[i][j] = mma_16x16x32<FMT>(b.a[i][h], b.x[j][h], acc[i][j]);
+                            for (int j = 0; j < TT; ++j) acc[i][j] = mma16<FMT>(b.a[i][h], b.x[j][h], acc[i][j]);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 };
@@ -363,8 +362,8 @@ constexpr float lift() { return FMT == WSR_BF16 ? 1.f : 2048.f; }
 /* c + w v_k, term k of the inner vectors. */
 template <int FMT>
 __device__ __forceinline__ f4_t accumulate(u32x4 w, u32x4 v, f4_t c, int k) {
-    if (FMT == WSR_BF16 || k == 0) return mma_16x16x32<FMT>(w, v, c);
-    const f4_t p = mma_16x16x32<FMT>(w, v, f4_t{0, 0, 0, 0});
+    if (FMT == WSR_BF16 || k == 0) return mma16<FMT>(w, v, c);
+    const f4_t p = mma16<FMT>(w, v, f4_t{0, 0, 0, 0});
 #pragma unroll
     for (int e = 0; e < 4; ++e) c[e] = fmaf(p[e], 1.f / lift<FMT>(), c[e]);
     return c;

@@ -1,23 +1,24 @@
 /*
  * wsr_step_device.h - device building blocks of the step operators (gfx950, wave64): 16-bit
- * conversions, wave and workgroup reductions, matrix instructions.
+ * conversions, wave and workgroup reductions, matrix instructions (16 x 16 x 32: wsr_mma.h).
  */
 #ifndef WSR_STEP_DEVICE_H
 #define WSR_STEP_DEVICE_H
 
-#include "wsr_device.h"
+#include "wsr_mma.h"
 #include "wsr_step_internal.h"
 
 namespace wsr_step {
 
+using wsr::b8_t;
+using wsr::f4_t;
+using wsr::h8_t;
+using wsr::mma16;
 using wsr::u32x4;
 using wsr::WAVE;
 
-typedef float f4_t __attribute__((ext_vector_type(4)));
 typedef float f16v_t __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
 typedef short s4_t __attribute__((ext_vector_type(4)));
 
 /* 16-byte loads and stores of fp32 rows that are only 4-byte aligned (the hardware takes them) */
@@ -87,6 +88,10 @@ __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+/* Until all of the wave's stores and atomics have arrived (vmcnt counts them beside the loads): those at agent scope, where
+   every XCD sees them. */
+__device__ __forceinline__ void wait_stores() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 /* v combined with its partner lane's v, by the levels of wsr::xchg_add: lane swaps for levels 0 and 1 (halves,
    then 16-lane rows), moves inside a 16-lane row for levels 2 to 5.  OP must not depend on the order of its
    operands; applied level by level it leaves the same bits in all lanes. */
@@ -126,16 +131,6 @@ __device__ __forceinline__ float row_sum(float v) {
 /* Over a wave. */
 __device__ __forceinline__ float wave_max(float v) { return row_max(xchg_max<1>(xchg_max<0>(v))); }
 __device__ __forceinline__ int wave_min(int v) { return row_min(xchg_min<1>(xchg_min<0>(v))); }
-
-/* D = A B + C on 16 x 16 x 32: lane l holds row l % 16 of A and column l % 16 of B, elements
-   8 (l / 16) .. + 7 of their 32; D's column l % 16, rows 4 (l / 16) .. + 3. */
-template <int FMT>
-__device__ __forceinline__ f4_t mma_16x16x32(u32x4 a, u32x4 b, f4_t c) {
-    if constexpr (FMT == WSR_BF16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8_t, a), __builtin_bit_cast(b8_t, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, a), __builtin_bit_cast(h8_t, b), c, 0, 0, 0);
-}
 
 /* D = A B + C on 32 x 32 x 16: lane l holds row l % 32 of A and column l % 32 of B, elements
    8 (l / 32) .. + 7 of their 16; D's column l % 32, register i row 8 (i / 4) + 4 (l / 32) + i % 4. */
