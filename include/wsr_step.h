@@ -145,8 +145,8 @@ wsr_status wsr_prefix_attention(const wsr_attn* p, void* ws, size_t ws_bytes, vo
    Sequence b has counts[b] drafted tokens (null: n_drafts), target logits in rows 0 .. counts[b] (row
    i: the distribution of the token after i accepted drafts) and the draft model's logits in rows
    0 .. counts[b] - 1 (draft null: each draft was looked up, its distribution all on that token).
-   With p = softmax(target / T), q = softmax(draft / T), T = temperature[b] (null: 1; T = 0: all on the
-   lowest index of the largest logit; above 1e30: 1e30), drafts are accepted in order while uniform_i * q_i(x_i) < p_i(x_i).
+   With p = softmax(target / T), q = softmax(draft / T), T = temperature[b] (null: 1; T = 0, and what is
+   not above 0: all on the lowest index of the largest logit; above 1e30: 1e30), drafts are accepted in order while uniform_i * q_i(x_i) < p_i(x_i).
    At the first refusal i, or after the last draft, the next token is the index with the largest
    w_v / noise_v (ties: the lowest), w = max(p_i - q_i, 0), after the last draft w = p (and where all
    of w is 0): with Exp(1) noise, a sample in proportion to w.

@@ -10,6 +10,11 @@
  *         layout of S^T is the operand layout of P^T when V's keys are taken in the same order, and
  *         V's transpose comes out of LDS by transposing reads (ds_read_b64_tr_b16).
  *
+ * P is rounded to the values' type: as two terms, which would leave the rounding of the output alone, the second
+ * product and its operands cost a third of the long cases (4 prompts of up to 900 behind 8192 357 us with one term, 481
+ * with two, error against 64 bits 0.0022 and 0.0017 relative; 24 sequences of 5 behind 32771 158 and 201; f16, 4 tokens
+ * behind 1024 10.3 and 10.7, 0.00025 and 0.00021).  The sum of a row's probabilities, the maximum and all sums are fp32.
+ *
  * Keys and values go from memory straight into LDS, two buffers, the next block in flight while one is
  * worked on; 16-byte pieces are placed so that reads meet no bank twice.
  *
