@@ -335,7 +335,8 @@ struct Attend {
     /* The products take masked keys with a probability of zero, and zero times an infinity or NaN among their values
        would reach rows that do not see them.  Such a row is found by its output (after join()) and summed up again,
        key by key over those it sees, against the maximum it has: nothing is paid for it in the loop (replacing such
-       values in LDS there cost 3 to 7 % of every call). */
+       values in LDS there cost 3 to 7 % of every call).  One with a NaN among its scores is NaN throughout and is left
+       alone (a NaN in one query's q, 63 tokens behind 4001 keys: summed up again 503 us, so 51, as without). */
     __device__ __forceinline__ bool broken() const {
         float z = 0.f;
 #pragma unroll
@@ -502,8 +503,8 @@ void k_attn(wsr_attn p, AttnPlan pl) {
     }
     a.join(lds, c, wave, lane);
     if (wave >= RW) return;
-    if (__ballot(a.broken()) && (!prefix || (k1 - k0) % A::KT)) {
-        const bool mine = a.broken();
+    const bool mine = a.broken() && a.l == a.l;                 /* a NaN sum makes all of the row NaN as it is */
+    if (__ballot(mine) && (!prefix || (k1 - k0) % A::KT)) {
         if (mine) a.clear();
 #pragma unroll 1
         for (int s = WHOLE ? 0 : !prefix; s <= (WHOLE ? 1 : !prefix); ++s) {
