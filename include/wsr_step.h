@@ -41,9 +41,9 @@ const char* wsr_step_last_error(void);
    where their pointers are null.  h' is stored to h_out (if not null) in fp32, x is rounded once to
    `fmt` (WSR_F16 or WSR_BF16), the type of w, b and gate too.  All arithmetic is fp32; an infinity or
    NaN in a token's inputs reaches that token's outputs only.
-   d % 8 == 0, d <= 32768, n_tokens < 2^31; rows and vectors 16-byte aligned, token strides multiples of 16.  gate:
-   one vector for all tokens (stride 0) or one per token.  h_out may be h itself (same stride);
-   outputs otherwise overlap nothing. */
+   d % 8 == 0, d <= 32768, n_tokens < 2^31; rows and vectors 16-byte aligned, token strides multiples of
+   16.  gate: one vector for all tokens (stride 0) or one per token.  h_out may be h itself (same
+   stride); outputs otherwise overlap nothing. */
 #define WSR_NORM_RMS 0
 #define WSR_NORM_LAYER 1
 #define WSR_BLOCK_POST 1
@@ -75,16 +75,16 @@ wsr_status wsr_block_norm(const wsr_block* p, void* stream);
    b + a * b_stride, both row-major in `fmt` (WSR_F16 or WSR_BF16), x in the same type, y and y0 fp32
    (y0 null: 0; y0 may be y itself with the same stride, the usual case after a sweep).  A token whose
    adapter is outside [0, n_adapters) has none: y = y0.  Products are exact, sums are fp32, and the
-   inner vector A x enters the second product with 24 bits (WSR_BF16), or with 22 (WSR_F16: entries down to
-   2^-28 of the token's largest; smaller ones within 2^-50 of it).  Rows of A and columns of B from r on are
-   not read.
+   inner vector A x enters the second product with 24 bits (WSR_BF16), or with 22 (WSR_F16: entries down
+   to 2^-28 of the token's largest; smaller ones within 2^-50 of it).  Rows of A and columns of B from r
+   on are not read.
    A projection with M = 0 does nothing and may have null pointers; with K = 0, a and x may be null.
    adapter_of: device int32 [n_tokens], in any order; ranks: device int32 [n_adapters], clamped to
    [0, rank], or null (all `rank`); scales: device fp32 [n_adapters] or null (all 1).
    K % 8 == 0, 1 <= rank <= 256; a, x 16-byte aligned, a_stride and x_tok_stride multiples of 16; b
    2-byte aligned; y, y0 4-byte aligned, strides multiples of 4, y_tok_stride >= 4 M for more than one
-   token.  n_tokens <= 2^20, n_adapters <= 8192, M < 2^31, K <= 2^28, 2^36 rows in all.  ws: wsr_lora_workspace_bytes(), 256-byte aligned,
-   read and written by this call only. */
+   token.  n_tokens <= 2^20, n_adapters <= 8192, M < 2^31, K <= 2^28, 2^36 rows in all.  ws:
+   wsr_lora_workspace_bytes(), 256-byte aligned, read and written by this call only. */
 typedef struct wsr_lora {
     int32_t fmt, rank;
     int64_t M, K;
@@ -111,17 +111,18 @@ wsr_status wsr_lora_sweep(const wsr_lora* mods, int32_t n, int32_t n_tokens, con
    of the prefix and its own keys j < lens[b] - n_b + i + 1:
      out = sum_k softmax_k(scale q . key_k) value_k,  lse = log sum_k exp(scale q . key_k).
    A row that sees no key gets out = 0 and lse = -inf, one with a NaN among its scores NaN in both.  Query
-   head h reads key head h / (n_heads / n_kv_heads).  Types `fmt` (WSR_F16 or WSR_BF16); scores, softmax statistics and sums
-   are fp32, probabilities are rounded to `fmt` for the product with the values, out once to `fmt`.
+   head h reads key head h / (n_heads / n_kv_heads).  Types `fmt` (WSR_F16 or WSR_BF16); scores, softmax
+   statistics and sums are fp32, probabilities are rounded to `fmt` for the product with the values, out
+   once to `fmt`.
    Keys past lens[b] are never read into a result (they may hold anything).  Rows of q that belong to no
    sequence (before starts[0], from starts[n_seqs] on) leave unspecified values in out and lse.
    starts: device int32 [n_seqs + 1], not decreasing, starts[n_seqs] <= n_tokens; lens: device int32
    [n_seqs], clamped to [0, max_len].  prefix_len and max_len at most 2^30, together at most 2^31 - 4096;
-   n_tokens and n_seqs at most 2^20, n_heads at most 4096, rows of a key head (tokens times its query heads) at
-   most 2^30; calls with n_kv_heads * (n_seqs + those rows / 128) past 2^22 may be refused.  head_dim 64 or 128; every pointer 16-byte
-   aligned and every stride a multiple of 16 (of 4 for lse); tok strides of keys at most 16 MiB; lse
-   (n_tokens, n_heads) or null.  k_prefix and v_prefix (k and v) have the same strides.  ws:
-   wsr_attn_workspace_bytes(), 256-byte aligned. */
+   n_tokens and n_seqs at most 2^20, n_heads at most 4096, rows of a key head (tokens times its query
+   heads) at most 2^30; calls with n_kv_heads * (n_seqs + those rows / 128) past 2^22 may be refused.
+   head_dim 64 or 128; every pointer 16-byte aligned and every stride a multiple of 16 (of 4 for lse);
+   tok strides of keys at most 16 MiB; lse (n_tokens, n_heads) or null.  k_prefix and v_prefix (k and v)
+   have the same strides.  ws: wsr_attn_workspace_bytes(), 256-byte aligned. */
 typedef struct wsr_attn {
     int32_t fmt, n_heads, n_kv_heads, head_dim, n_seqs, n_tokens;
     float scale;
@@ -146,7 +147,8 @@ wsr_status wsr_prefix_attention(const wsr_attn* p, void* ws, size_t ws_bytes, vo
    i: the distribution of the token after i accepted drafts) and the draft model's logits in rows
    0 .. counts[b] - 1 (draft null: each draft was looked up, its distribution all on that token).
    With p = softmax(target / T), q = softmax(draft / T), T = temperature[b] (null: 1; T = 0, and what is
-   not above 0: all on the lowest index of the largest logit; above 1e30: 1e30), drafts are accepted in order while uniform_i * q_i(x_i) < p_i(x_i).
+   not above 0: all on the lowest index of the largest logit; above 1e30: 1e30), drafts are accepted in
+   order while uniform_i * q_i(x_i) < p_i(x_i).
    At the first refusal i, or after the last draft, the next token is the index with the largest
    w_v / noise_v (ties: the lowest), w = max(p_i - q_i, 0), after the last draft w = p (and where all
    of w is 0): with Exp(1) noise, a sample in proportion to w.
@@ -157,8 +159,8 @@ wsr_status wsr_prefix_attention(const wsr_attn* p, void* ws, size_t ws_bytes, vo
    with no token that can be drawn accepts nothing and gives token -1 with logp -inf, and so does a
    draft outside [0, vocab) count as refused.
    target, draft: fp32, strides multiples of 4, rows 4-byte aligned; tokens: int32 (n_seqs, n_drafts);
-   uniform: fp32 (n_seqs, n_drafts) in [0, 1); noise: fp32 (n_seqs, vocab), positive and normal;
-   counts, temperature: device [n_seqs], counts clamped to [0, n_drafts].  1 <= vocab <= 2^24,
+   uniform: fp32 (n_seqs, n_drafts) in [0, 1); noise: fp32 (n_seqs, vocab), from 2^-126 to
+   2^100; counts, temperature: device [n_seqs], counts clamped to [0, n_drafts].  1 <= vocab <= 2^24,
    0 <= n_drafts <= 63, n_seqs <= 2^16.  ws: wsr_verify_workspace_bytes(), 256-byte aligned. */
 typedef struct wsr_verify {
     int32_t n_seqs, n_drafts;
