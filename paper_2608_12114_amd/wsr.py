@@ -242,17 +242,25 @@ _STEP_NAMES = frozenset((
     "WSR_NORM_RMS", "WSR_NORM_LAYER", "WSR_BLOCK_POST", "wsr_block", "wsr_lora", "wsr_attn", "wsr_verify", "make_block", "make_loras",
     "make_attn", "make_verify", "step_lib", "wsr_step_last_error", "wsr_block_norm", "wsr_lora_workspace_bytes", "wsr_lora_sweep",
     "wsr_attn_workspace_bytes", "wsr_prefix_attention", "wsr_verify_workspace_bytes", "wsr_verify_drafts"))
+_SERVE_NAMES = frozenset((
+    "WSR_QKV_NORM", "WSR_QKV_PAIRS", "wsr_pages", "wsr_qkv", "wsr_paged", "wsr_logprobs", "make_pages", "make_qkv", "make_paged",
+    "make_logprobs", "serve_lib", "wsr_serve_last_error", "wsr_append_qkv", "wsr_paged_workspace_bytes", "wsr_paged_attention",
+    "wsr_logprobs_workspace_bytes", "wsr_token_logprobs"))
 
 
 def __getattr__(name):
     """The entry points of include/wsr_step.h (wsr_block_norm, wsr_lora_sweep, wsr_prefix_attention,
-    wsr_verify_drafts and what belongs to them), from the binding of libwsr_step.so: loaded on first use.
-    Any other name, and these where that library is not built, is an AttributeError."""
-    if name not in _STEP_NAMES:
-        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    wsr_verify_drafts and what belongs to them) and of include/wsr_serve.h (wsr_append_qkv, wsr_paged_attention,
+    wsr_token_logprobs), from the bindings of libwsr_step.so and libwsr_serve.so: loaded on first use.
+    Any other name, and these where their library is not built, is an AttributeError."""
     try:
-        from . import wsr_step
+        if name in _STEP_NAMES:
+            from . import wsr_step as binding
+        elif name in _SERVE_NAMES:
+            from . import wsr_serve as binding
+        else:
+            raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
     except ImportError as e:
         raise AttributeError(f"{name}: {e}") from e
-    value = globals()[name] = getattr(wsr_step, name)
+    value = globals()[name] = getattr(binding, name)
     return value
