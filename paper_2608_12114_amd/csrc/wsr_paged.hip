@@ -490,7 +490,7 @@ __global__ __launch_bounds__(AT) void k_paged_join(wsr_paged p, PagedPlan pl, in
     const int lane = threadIdx.x % WAVE;
     if (at >= (int64_t)p.n_tokens * p.n_heads) return;
     const int tok = (int)(at / p.n_heads), qh = (int)(at % p.n_heads), G = p.n_heads / p.n_kv_heads, R = pl.rows;
-    const int b = seq_of(p.starts, p.n_seqs, tok);
+    const int b = seq_of(p.starts, p.n_seqs, tok).seq;
     if (b < 0) return;
     const Line line = line_of(p, pl, lane);
     int64_t x = 0;

@@ -22,24 +22,33 @@ using wsr_step::unpack8;
 constexpr float NEG_INF = -__builtin_inff();
 constexpr float LOG2E = 1.4426950408889634f;
 
-/* The sequence that row `tok` belongs to, -1 where there is none: the last that starts at or before it, by a search of 64
-   samples at a time (one load's latency up to 64 sequences, two up to 4096).  By whole waves, tok uniform. */
-__device__ __forceinline__ int seq_of(const int32_t* starts, int n_seqs, int tok) {
-    if (!starts) return tok < n_seqs ? tok : -1;
+/* The sequence that row `tok` belongs to (-1: none) and the row behind its last: the last sequence that starts at or before
+   it, by a search of 64 samples at a time (one load's latency below 64 sequences, two below 4096).  By whole waves, tok
+   uniform. */
+struct Belongs {
+    int seq, end;
+};
+__device__ __forceinline__ Belongs seq_of(const int32_t* starts, int n_seqs, int tok) {
+    if (!starts) return Belongs{tok < n_seqs ? tok : -1, tok + 1};
     const int lane = threadIdx.x % WAVE;
     int lo = 0, n = n_seqs + 1;               /* how many start at or before tok: lo to lo + n */
+    int first = 0, end = 0;                   /* starts[lo - 1] and, where it was among the samples, starts[lo] */
+    bool ended = false;
     while (n > 0) {
-        const int step = (n + WAVE - 1) / WAVE;
-        const int at = lane * step;
-        const bool in = at < n && starts[lo + at] <= tok;
-        const int c = __builtin_popcountll(__ballot(in));
+        const int step = (n + WAVE - 1) / WAVE, at = lane * step, all = (n + step - 1) / step;
+        const int v = at < n ? starts[lo + at] : 0;
+        const int c = __builtin_popcountll(__ballot(at < n && v <= tok));
         if (c == 0) break;
+        first = __builtin_amdgcn_readlane(v, c - 1);
+        ended = step == 1 && c < all;
+        if (ended) end = __builtin_amdgcn_readlane(v, c);
         lo += (c - 1) * step + 1;
         n = min(step - 1, n - (c - 1) * step - 1);
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
-    if (lo < 1 || lo > n_seqs) return -1;
-    return starts[lo - 1] <= tok && tok < starts[lo] ? lo - 1 : -1;
+    if (lo < 1 || lo > n_seqs) return Belongs{-1, 0};
+    if (!ended) end = starts[lo];
+    return Belongs{first <= tok && tok < end ? lo - 1 : -1, end};
 }
 
 /* The page of a place, and whether it is one. */
