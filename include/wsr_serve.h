@@ -132,7 +132,8 @@ wsr_status wsr_paged_attention(const wsr_paged* p, void* ws, size_t ws_bytes, vo
    logp -inf and rank -1.  A row with fewer than n_top tokens that can be drawn ends with token -1 and logp -inf; a row
    with none has entropy 0.
    logits: fp32, 4-byte aligned, row_stride a multiple of 4; tokens: device int32 [n_rows] or null (no logp, no rank);
-   logp, rank, entropy and top_logp may be null.  1 <= vocab <= 2^24, 0 <= n_top <= 64, n_rows <= 2^20.
+   logp, rank, entropy and top_logp may be null.  1 <= vocab <= 2^24, 0 <= n_top <= 64, n_rows <= 2^20,
+   n_rows * vocab <= 2^40.
    ws: wsr_logprobs_workspace_bytes(), 256-byte aligned. */
 typedef struct wsr_logprobs {
     int64_t n_rows, vocab;

@@ -4,13 +4,15 @@
  *   p = softmax(l / T):  log p_x = (l_x - m) / T - log s,  s = sum exp((l - m) / T),
  *   entropy = log s + sum p (m - l) / T
  *
- * One read of a row: every lane keeps a maximum of its own, the two sums against it, and how many logits come before the
- * given token's.  A row is a workgroup's, or, where rows are few, several parts' that a second launch joins.
+ * One read of a row: every lane keeps a maximum of its own and the two sums against it, and the wave how many logits come
+ * before the given token's.  All rows' chunks lie on one line of which every workgroup takes an equal share, so that any
+ * number of rows fills the chip; rows that lie in several shares are joined in a second launch.
  *
  * The n largest: a wave keeps its best 64 in order, one per lane, as 64-bit keys (the logit's bits in an order of whole
  * numbers, then the index from the top, so that equal logits go by index).  Logits that pass the n-th key, which after
  * the first few hundred are rare, are collected in LDS and merged in 64 at a time, sorted by compare-and-swap networks
- * over the wave.  The first chunk's threshold is the n-th largest of the lanes' maxima, which n logits reach.
+ * over the wave.  The first chunk's threshold is the n-th largest of the lanes' maxima, which n logits reach.  A single
+ * alternative is a lane's largest and needs none of this.
  *
  * exp((l - m) / T) is taken as exp2((l - m) * (log2 e / T)): one rounding of the product, 2^-24 |l - m| / T relative.
  */
@@ -25,19 +27,32 @@ namespace wsr_serve {
 constexpr int LT = 256, LW = LT / WAVE;       /* threads, waves */
 typedef uint64_t key64;
 
-struct LogPlan {
-    int32_t parts, per;                       /* of a row, and chunks of a part */
-    key64* keys;                              /* [n_rows][parts][n_top] */
-    struct LogStat* stats;                    /* [n_rows][parts] */
-};
 struct LogStat {
     float m, s, e;                            /* largest logit; sums of 2^x and of x 2^x, x = (l - m) log2 e / T */
-    int32_t before;
+    float mine;                               /* the given token's logit, and whether there is one; logits before it */
+    int32_t ranked, before;
+};
+struct LogPlan {
+    uint32_t all, chunks;                     /* chunks of the line (at most 2^32 - 1), and of a row */
+    int32_t shares;
+    uint32_t each, rest;                      /* all / shares, all % shares */
+    key64* keys;                              /* [2 * shares][n_top] */
+    LogStat* stats;                           /* [2 * shares] */
+    /* Share w's first chunk.  A row that lies in several shares leaves a part in each: the first in slot 2 w + 1, the others
+       in 2 w. */
+    __device__ __forceinline__ uint32_t start(int w) const { return each * w + rest * w / shares; }
+    __device__ __forceinline__ int share_of(uint32_t x) const {
+        int w = min((int)((double)x / (double)all * shares), shares - 1);
+        while (w > 0 && start(w) > x) --w;
+        while (w + 1 < shares && start(w + 1) <= x) ++w;
+        return w;
+    }
 };
 
-__device__ __forceinline__ float no_nan(float v) { return v == v ? v + 0.f : NEG_INF; }     /* and -0 is 0 */
+/* NaN counts as -inf. */
+__device__ __forceinline__ float no_nan(float v) { return fmaxf(v, NEG_INF); }
 __device__ __forceinline__ key64 key_of(float v, int i) {
-    const uint32_t b = __float_as_uint(v);
+    const uint32_t b = __float_as_uint(v + 0.f);                /* -0 is 0 */
     return (key64)(b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u)) << 32 | (0xffffffffu - (uint32_t)i);
 }
 __device__ __forceinline__ float logit_of(key64 k) {
@@ -50,6 +65,7 @@ __device__ __forceinline__ float temperature_of(const wsr_logprobs& p, int64_t r
     const float t = p.temperature ? p.temperature[r] : 1.f;
     return t > 0.f ? fminf(t, 1e30f) : 0.f;
 }
+__device__ __forceinline__ float factor_of(float t) { return t > 0.f ? LOG2E / t : 0.f; }
 
 /* s, e against m, moved to the maximum `to` >= m. */
 __device__ __forceinline__ void move_max(float& m, float& s, float& e, float to, float k) {
@@ -59,41 +75,114 @@ __device__ __forceinline__ void move_max(float& m, float& s, float& e, float to,
     s = f > 0.f ? s * f : 0.f;
     m = to;
 }
+__device__ __forceinline__ void join_stats(LogStat& a, LogStat b, float k) {
+    const float top = fmaxf(a.m, b.m);
+    move_max(a.m, a.s, a.e, top, k);
+    move_max(b.m, b.s, b.e, top, k);
+    a.s += b.s, a.e += b.e, a.before += b.before;
+}
 
-__device__ __forceinline__ key64 shfl_xor(key64 v, int d) { return __shfl_xor((unsigned long long)v, d); }
+/* ---- sorting networks over a wave: one key per lane ---------------------------------------------------- */
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+}
+/* The value of lane i ^ D. */
+template <int D>
+__device__ __forceinline__ uint32_t other(uint32_t v) {
+    if constexpr (D == 1) return moved<wsr::DPP_XOR1>(v);
+    else if constexpr (D == 2) return moved<wsr::DPP_XOR2>(v);
+    else if constexpr (D == 4) return moved<0x1B>(moved<wsr::DPP_HALF_MIRROR>(v));      /* i ^ 7, then i ^ 3 */
+    else if constexpr (D == 8) return moved<0x128>(v);          /* a 16-lane row turned by 8 */
+    else {
+        const bool upper = threadIdx.x & D;
+        if constexpr (D == 16) {
+            const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+            return upper ? s[0] : s[1];
+        } else {
+            const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+            return upper ? s[0] : s[1];
+        }
+    }
+}
+template <int D>
+__device__ __forceinline__ float other(float v) { return __uint_as_float(other<D>(__float_as_uint(v))); }
+template <int D>
+__device__ __forceinline__ key64 other(key64 v) { return (key64)other<D>((uint32_t)(v >> 32)) << 32 | other<D>((uint32_t)v); }
+
+/* One level: the larger of the two in the lower lane where `down`. */
+template <int D, typename T>
+__device__ __forceinline__ T level(T v, bool down, int lane) {
+    const T o = other<D>(v);
+    return (((lane & D) == 0) == down) == (v > o) ? v : o;
+}
+/* N lanes each of a bitonic sequence put in falling (rising) order. */
+template <int N, typename T>
+__device__ __forceinline__ T merged(T v, bool down, int lane) {
+    if constexpr (N >= 64) v = level<32>(v, down, lane);
+    if constexpr (N >= 32) v = level<16>(v, down, lane);
+    if constexpr (N >= 16) v = level<8>(v, down, lane);
+    if constexpr (N >= 8) v = level<4>(v, down, lane);
+    if constexpr (N >= 4) v = level<2>(v, down, lane);
+    return level<1>(v, down, lane);
+}
+/* Whether group lane / N of the wave is an even one; of the whole wave, `last`. */
+template <int N>
+__device__ __forceinline__ bool even(int lane, bool last) { return N >= WAVE ? last : (lane & N) == 0; }
+/* Groups of W lanes put in falling order where they are even, rising where odd; the whole wave falling where `last`. */
+template <int W, typename T>
+__device__ __forceinline__ T sorted(T v, bool last, int lane) {
+    if constexpr (W >= 2) v = merged<2>(v, even<2>(lane, last), lane);
+    if constexpr (W >= 4) v = merged<4>(v, even<4>(lane, last), lane);
+    if constexpr (W >= 8) v = merged<8>(v, even<8>(lane, last), lane);
+    if constexpr (W >= 16) v = merged<16>(v, even<16>(lane, last), lane);
+    if constexpr (W >= 32) v = merged<32>(v, even<32>(lane, last), lane);
+    if constexpr (W >= 64) v = merged<64>(v, last, lane);
+    return v;
+}
+/* The W largest of the wave, from groups that sorted() put in order: in every group, falling where `last`, else rising. */
+template <int W, int D = W, typename T>
+__device__ __forceinline__ T largest(T v, bool last, int lane) {
+    if constexpr (D >= WAVE) return v;
+    else {
+        v = std::max(v, other<D>(v));
+        if constexpr (W > 1) v = merged<W>(v, even<2 * D>(lane, last), lane);
+        return largest<W, 2 * D>(v, last, lane);
+    }
+}
+/* The W largest of `count` falling lists of W, in every group, falling.  at(i, j): entry j of list i (0 past the lists). */
+template <int W, int STEP, typename F>
+__device__ __forceinline__ key64 largest_of(int count, int lane, const F& at) {
+    constexpr int G = WAVE / W, AHEAD = 4;
+    const int g = lane / W, j = lane % W;
+    const bool down = even<W>(lane, true);
+    key64 best = 0;
+    for (int i0 = 0; i0 < count; i0 += AHEAD * G * STEP) {
+        key64 o[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) o[a] = at(i0 + (a * G + g) * STEP, down ? W - 1 - j : j);
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a)
+            if (i0 + a * G * STEP < count) {
+                best = std::max(best, o[a]);
+                if constexpr (W > 1) best = merged<W>(best, down, lane);
+            }
+    }
+    return largest<W>(best, true, lane);
+}
 __device__ __forceinline__ key64 lane_key(key64 v, int lane) {
     return (key64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
 }
-
-/* One level of a sorting network: the larger of the two in the lower lane where `down`. */
-__device__ __forceinline__ key64 level(key64 v, int d, bool down, int lane) {
-    const key64 o = shfl_xor(v, d);
-    return (((lane & d) == 0) == down) == (v > o) ? v : o;
-}
-/* A bitonic sequence put in falling order. */
-__device__ __forceinline__ key64 fall(key64 v, int lane) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v = level(v, d, true, lane);
-    return v;
-}
-/* Rising (falling) order over the wave. */
-template <bool DOWN>
-__device__ __forceinline__ key64 sorted(key64 v, int lane) {
-#pragma unroll
-    for (int n = 2; n <= WAVE; n <<= 1)
-#pragma unroll
-        for (int d = n / 2; d; d >>= 1) v = level(v, d, n == WAVE ? DOWN : ((lane & n) == 0) == DOWN, lane);
-    return v;
-}
-
 /* The wave's LDS stores are there for its loads that follow. */
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
 
-constexpr int ROOM = 9 * WAVE;                /* up to 63 that wait and eight of each lane */
+constexpr int ROOM = 5 * WAVE;                /* up to 63 that wait and four of each lane */
 
-/* The best of a wave, and what waits to be merged into it. */
+/* The best W of a wave, and what waits to be merged into it. */
+template <int W>
 struct Best {
-    key64 best, least;                        /* this lane's; the n-th, which others have to pass */
+    key64 best, least;                        /* this lane's, falling in every group of W; the n-th, which others have to pass */
     float bar;                                /* its logit, -inf at the start */
     int waiting, n;
     key64* room;                              /* [ROOM] in LDS */
@@ -103,8 +192,8 @@ struct Best {
         if (k > least) least = k, bar = logit_of(k);
     }
     __device__ __forceinline__ void merge(key64 v, int lane) {
-        const key64 r = sorted<false>(v, lane);
-        best = fall(best > r ? best : r, lane);
+        const key64 r = largest<W>(sorted<W>(v, false, lane), false, lane);
+        best = merged<W>(std::max(best, r), true, lane);
         raise(lane_key(best, n - 1));
     }
     /* Keys that pass `least` (or are it) of all lanes wait in the room, ... */
@@ -127,12 +216,13 @@ struct Best {
         wave_fence();
         if (waiting) merge(lane < waiting ? room[lane] : 0, lane);
         waiting = 0;
+        wave_fence();
     }
 };
 
 /* What is stored for a row, by one wave: its statistics and best keys. */
-__device__ __forceinline__ void finish(const wsr_logprobs& p, int64_t r, const LogStat& st, key64 best, int lane) {
-    const float t = temperature_of(p, r), log_s = logf(st.s);
+__device__ __forceinline__ void finish(const wsr_logprobs& p, int64_t r, float t, const LogStat& st, key64 best, int lane) {
+    const float log_s = logf(st.s);
     auto log_prob = [&](float l, bool first) {
         if (!(l > NEG_INF)) return NEG_INF;
         if (t == 0.f) return first ? 0.f : NEG_INF;
@@ -143,167 +233,213 @@ __device__ __forceinline__ void finish(const wsr_logprobs& p, int64_t r, const L
         if (p.top_logp) p.top_logp[r * p.n_top + lane] = best ? log_prob(logit_of(best), lane == 0) : NEG_INF;
     }
     if (lane) return;
+    if (p.logp) p.logp[r] = st.ranked ? log_prob(st.mine, st.before == 0) : NEG_INF;
+    if (p.rank) p.rank[r] = st.ranked ? st.before : -1;
     if (p.entropy) p.entropy[r] = t == 0.f || st.m == NEG_INF ? 0.f : fmaxf(log_s - 0.6931471805599453f * (st.e / st.s), 0.f);
-    if (p.tokens) {
-        const int x = p.tokens[r];
-        const bool in = x >= 0 && x < p.vocab;
-        const float l = in ? no_nan(((const float*)((const char*)p.logits + r * p.row_stride))[x]) : NEG_INF;
-        if (p.logp) p.logp[r] = log_prob(l, st.before == 0);
-        if (p.rank) p.rank[r] = in ? st.before : -1;
-    }
 }
 
-/* TOP: whether alternatives are asked for. */
-template <int VU, bool TOP>                   /* VU: 16-byte loads per thread, even */
-__global__ __launch_bounds__(LT) void k_logprobs(wsr_logprobs p, LogPlan pl) {
+/* TOP: no alternatives, one, or up to 8, 32 or 64.  VU: 16-byte loads per thread of a chunk. */
+template <int VU, int TOP>
+__global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_logprobs(wsr_logprobs p, LogPlan pl) {
     constexpr int CHUNK = LT * VU * 4;
-    __shared__ key64 room[LW][ROOM];
-    __shared__ LogStat sums[LW];
-    const int64_t r = blockIdx.x / pl.parts;
-    const int part = blockIdx.x % pl.parts, lane = threadIdx.x % WAVE, wave = wsr::wave_in_block();
-    const float* row = (const float*)((const char*)p.logits + r * p.row_stride);
-    const int n = (int)p.vocab, from = part * pl.per * CHUNK, to = (int)std::min<int64_t>((int64_t)from + (int64_t)pl.per * CHUNK, n);
-    const float t = temperature_of(p, r), k = t > 0.f ? LOG2E / t : 0.f;
-    const int token = p.tokens ? p.tokens[r] : -1;
-    const bool ranked = token >= 0 && token < n;
-    const float mine = ranked ? no_nan(row[token]) : 0.f;
-    float m = NEG_INF, s = 0.f, e = 0.f;
-    int before = 0;
-    Best b;
-    b.init(room[wave], p.n_top);
-    auto load = [&](int at, float (&v)[VU][4]) __attribute__((always_inline)) {
+    __shared__ key64 room[TOP > 1 ? LW : 1][ROOM];
+    __shared__ key64 lists[2][LW][TOP > 0 ? TOP : 1];          /* by the parity of the part, so that one barrier a part is enough */
+    __shared__ LogStat sums[2][LW];
+    const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), n = (int)p.vocab;
+    uint32_t at = pl.start(blockIdx.x);
+    const uint32_t end = pl.start(blockIdx.x + 1);
+    if (at >= end) return;
+    int64_t r = at / pl.chunks;
+    const int chunks = (int)pl.chunks;
+    int c = (int)(at % pl.chunks);
+    const char* row = (const char*)p.logits + r * p.row_stride;
+    float next[VU][4];
+    auto load = [&](const float* from, int chunk) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < VU; ++u) {
-            const int i = at + (u * LT + (int)threadIdx.x) * 4;
-            if (i + 4 <= to) {
-                const f4_t q = *(const wsr_step::f4_any_t*)(row + i);
+            const int i = chunk * CHUNK + (u * LT + (int)threadIdx.x) * 4;
+            if (i + 4 <= n) {
+                const f4_t q = *(const wsr_step::f4_any_t*)(from + i);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[u][j] = no_nan(q[j]);
+                for (int j = 0; j < 4; ++j) next[u][j] = q[j];
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[u][j] = i + j < to ? no_nan(row[i + j]) : NEG_INF;
+                for (int j = 0; j < 4; ++j) next[u][j] = i + j < n ? from[i + j] : NEG_INF;
             }
         }
     };
-    for (int at = from; at < to; at += CHUNK) {
-        float v[VU][4];
-        load(at, v);
-        const int i0 = at + (int)threadIdx.x * 4;
-        float top = v[0][0];
+    int token = p.tokens ? p.tokens[r] : -1;
+    float t = temperature_of(p, r);
+    load((const float*)row, c);
+    Best<(TOP > 1 ? TOP : 2)> b;
+    /* a part: chunks of one row */
+#pragma unroll 1
+    for (int parity = 0; at < end; parity ^= 1) {
+        const bool head = c == 0;
+        const float k = factor_of(t);
+        const bool ranked = token >= 0 && token < n;
+        const float mine = ranked ? no_nan(((const float*)row)[token]) : __builtin_inff();
+        float m = NEG_INF, s = 0.f, e = 0.f, one = NEG_INF;
+        int before = 0, one_at = 0x7fffffff;
+        if constexpr (TOP > 1) b.init(room[wave], p.n_top);
+#pragma unroll 1
+        for (bool first = true; at < end && c < chunks; first = false, ++at, ++c) {
+            float v[VU][4];
 #pragma unroll
-        for (int u = 0; u < VU; ++u)
+            for (int u = 0; u < VU; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top = fmaxf(top, v[u][j]);
-        if (top > m) move_max(m, s, e, top, k);
+                for (int j = 0; j < 4; ++j) v[u][j] = no_nan(next[u][j]);
+            if (at + 1 < end) load((const float*)(c + 1 < chunks ? row : row + p.row_stride), c + 1 < chunks ? c + 1 : 0);
+            const int i0 = c * CHUNK + (int)threadIdx.x * 4;
+            float top = v[0][0];
 #pragma unroll
-        for (int u = 0; u < VU; ++u)
+            for (int u = 0; u < VU; ++u)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float l = v[u][j], x = l == m ? 0.f : (l - m) * k, f = __builtin_amdgcn_exp2f(x);
-                s += l > NEG_INF ? f : 0.f;
-                e += l > NEG_INF && f > 0.f ? f * x : 0.f;
-                before += l > mine || (l == mine && i0 + u * LT * 4 + j < token);
+                for (int j = 0; j < 4; ++j) top = fmaxf(top, v[u][j]);
+            if (top > m) move_max(m, s, e, top, k);
+            if (__ballot(m == __builtin_inff())) {
+#pragma unroll
+                for (int u = 0; u < VU; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float x = v[u][j] == m ? 0.f : fmaxf((v[u][j] - m) * k, -200.f), f = v[u][j] > NEG_INF ? __builtin_amdgcn_exp2f(x) : 0.f;
+                        s += f;
+                        e = fmaf(f, x, e);
+                    }
+            } else {
+                /* -inf gives 2^-200, which is 0, and 0 times -200 */
+                const float base = m == NEG_INF ? 0.f : m;
+#pragma unroll
+                for (int u = 0; u < VU; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float x = fmaxf((v[u][j] - base) * k, -200.f), f = __builtin_amdgcn_exp2f(x);
+                        s += f;
+                        e = fmaf(f, x, e);
+                    }
             }
-        if constexpr (TOP) {
-            if (at == from) {
-                /* the first of a lane's that has its largest, so that equal logits raise no bar above themselves */
-                key64 first = 0;
+            /* logits before the given token come before it where they equal its, those behind it do not */
+            if (c * CHUNK + CHUNK <= token) {
+#pragma unroll
+                for (int u = 0; u < VU; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) before += __builtin_popcountll(__ballot(v[u][j] >= mine));
+            } else if (c * CHUNK > token) {
+#pragma unroll
+                for (int u = 0; u < VU; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) before += __builtin_popcountll(__ballot(v[u][j] > mine));
+            } else {
 #pragma unroll
                 for (int u = 0; u < VU; ++u)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (v[u][j] > NEG_INF) first = std::max(first, key_of(v[u][j], i0 + u * LT * 4 + j));
-                b.raise(lane_key(sorted<true>(first, lane), b.n - 1));
+                        before += __builtin_popcountll(__ballot(v[u][j] > mine || (v[u][j] == mine && i0 + u * LT * 4 + j < token)));
             }
-            if (__ballot(top >= b.bar && top > NEG_INF))
+            if constexpr (TOP == 1) {
+                if (__ballot(top > one))
 #pragma unroll
-                for (int u = 0; u < VU; ++u) {
+                    for (int u = 0; u < VU; ++u)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) b.add(key_of(v[u][j], i0 + u * LT * 4 + j), v[u][j] > NEG_INF, lane);
-                    if (u % 2) b.drain(lane);
+                        for (int j = 0; j < 4; ++j)
+                            if (v[u][j] > one) one = v[u][j], one_at = i0 + u * LT * 4 + j;
+            }
+            if constexpr (TOP > 1) {
+                if (first) {
+                    const float bar = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sorted<WAVE>(top, true, lane)), p.n_top - 1));
+                    if (bar > NEG_INF) b.raise(key_of(bar, -1));
                 }
-        }
-    }
-    /* a wave's, then the workgroup's */
-    const float wm = wsr_step::wave_max(m);
-    move_max(m, s, e, wm, k);
-    s = wsr::wave_sum(s), e = wsr::wave_sum(e);
+                if (__ballot(top >= b.bar && top > NEG_INF))
 #pragma unroll
-    for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d);
-    if constexpr (TOP) {
-        b.flush(lane);
-        wave_fence();
-        room[wave][lane] = b.best;
-    }
-    if (lane == 0) sums[wave] = LogStat{m, s, e, before};
-    __syncthreads();
-    if (wave) return;
-    LogStat st = sums[0];
-    for (int w = 1; w < LW; ++w) {
-        LogStat o = sums[w];
-        const float top = fmaxf(st.m, o.m);
-        move_max(st.m, st.s, st.e, top, k);
-        move_max(o.m, o.s, o.e, top, k);
-        st.s += o.s, st.e += o.e, st.before += o.before;
-    }
-    if constexpr (TOP)
+                    for (int u = 0; u < VU; ++u) {
 #pragma unroll
-        for (int w = 1; w < LW; ++w) {
-            const key64 o = room[w][WAVE - 1 - lane];
-            b.best = fall(b.best > o ? b.best : o, lane);
+                        for (int j = 0; j < 4; ++j) b.add(key_of(v[u][j], i0 + u * LT * 4 + j), v[u][j] > NEG_INF, lane);
+                        b.drain(lane);
+                    }
+            }
         }
-    if (pl.parts == 1) {
-        finish(p, r, st, b.best, lane);
-    } else {
-        const int64_t at = r * pl.parts + part;
-        if (TOP && lane < p.n_top) pl.keys[at * p.n_top + lane] = b.best;
-        if (lane == 0) pl.stats[at] = st;
+        /* a wave's results, then the workgroup's */
+        move_max(m, s, e, wsr_step::wave_max(m), k);
+        s = wsr::wave_sum(s), e = wsr::wave_sum(e);
+        if constexpr (TOP == 1) {
+            const float top = wsr_step::wave_max(one);
+            const int where = wsr_step::wave_min(one == top ? one_at : 0x7fffffff);
+            if (lane == 0) lists[parity][wave][0] = top > NEG_INF ? key_of(top, where) : 0;
+        }
+        if constexpr (TOP > 1) {
+            b.flush(lane);
+            if (lane < TOP) lists[parity][wave][lane] = b.best;
+        }
+        if (lane == 0) sums[parity][wave] = LogStat{m, s, e, mine, ranked, before};
+        __syncthreads();
+        if (wave == 0) {
+            LogStat st = sums[parity][0];
+            for (int w = 1; w < LW; ++w) join_stats(st, sums[parity][w], k);
+            key64 best = 0;
+            if constexpr (TOP > 0) best = largest_of<TOP, 1>(LW, lane, [&](int i, int j) { return i < LW ? lists[parity][i][j] : 0; });
+            if (head && c == chunks) {
+                finish(p, r, t, st, best, lane);
+            } else {
+                const int64_t slot = 2 * (int64_t)blockIdx.x + head;
+                if (TOP && lane < p.n_top) pl.keys[slot * p.n_top + lane] = best;
+                if (lane == 0) pl.stats[slot] = st;
+            }
+        }
+        if (c < chunks || at >= end) break;
+        c = 0, ++r, row += p.row_stride;
+        token = p.tokens ? p.tokens[r] : -1;
+        t = temperature_of(p, r);
     }
 }
 
-/* A row's parts, by one wave. */
-__global__ __launch_bounds__(WAVE) void k_logprobs_join(wsr_logprobs p, LogPlan pl) {
-    __shared__ key64 room[2 * WAVE];      /* one key of each lane at a time */
-    const int64_t r = blockIdx.x;
-    const int lane = threadIdx.x;
-    const float t = temperature_of(p, r), k = t > 0.f ? LOG2E / t : 0.f;
-    LogStat st{NEG_INF, 0.f, 0.f, 0};
-    for (int c = lane; c < pl.parts; c += WAVE) {
-        LogStat o = pl.stats[r * pl.parts + c];
-        const float top = fmaxf(st.m, o.m);
-        move_max(st.m, st.s, st.e, top, k);
-        move_max(o.m, o.s, o.e, top, k);
-        st.s += o.s, st.e += o.e, st.before += o.before;
-    }
-    move_max(st.m, st.s, st.e, wsr_step::wave_max(st.m), k);
+/* Rows that lie in several shares, by the share that the first border inside them ends; a wave takes every fourth part. */
+template <int TOP>
+__global__ __launch_bounds__(LT) void k_logprobs_join(wsr_logprobs p, LogPlan pl) {
+    __shared__ key64 lists[LW][TOP > 0 ? TOP : 1];
+    __shared__ LogStat sums[LW];
+    const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), w0 = blockIdx.x;
+    const uint32_t border = pl.start(w0 + 1), row0 = border / pl.chunks * pl.chunks;
+    if (border == row0 || pl.start(w0) > row0) return;
+    const int64_t r = row0 / pl.chunks;
+    const int parts = pl.share_of(row0 + pl.chunks - 1) - w0 + 1;
+    auto slot = [&](int i) { return 2 * (int64_t)(w0 + i) + (i == 0); };
+    const float t = temperature_of(p, r), k = factor_of(t);
+    LogStat st = pl.stats[slot(0)];
+    if (threadIdx.x) st.m = NEG_INF, st.s = 0.f, st.e = 0.f, st.before = 0;
+    for (int i = threadIdx.x ? threadIdx.x : LT; i < parts; i += LT) join_stats(st, pl.stats[slot(i)], k);
+    key64 best = 0;
+    if constexpr (TOP > 0)
+        best = largest_of<TOP, LW>(parts - wave, lane, [&](int i, int j) {
+            return i + wave < parts && j < p.n_top ? pl.keys[slot(i + wave) * p.n_top + j] : 0;
+        });
+    const float top = wsr_step::wave_max(st.m);
+    move_max(st.m, st.s, st.e, top, k);
     st.s = wsr::wave_sum(st.s), st.e = wsr::wave_sum(st.e);
 #pragma unroll
     for (int d = 32; d; d >>= 1) st.before += __shfl_xor(st.before, d);
-    Best b;
-    b.init(room, p.n_top);
-    const key64* keys = pl.keys + r * pl.parts * p.n_top;
-    const int all = pl.parts * p.n_top;
-    for (int i = 0; i < all; i += WAVE) {
-        const key64 v = i + lane < all ? keys[i + lane] : 0;
-        b.add(v, v != 0, lane);
-        b.drain(lane);
-    }
-    b.flush(lane);
-    finish(p, r, st, b.best, lane);
+    if (lane == 0) sums[wave] = st;
+    if (TOP > 0 && lane < TOP) lists[wave][lane] = best;
+    __syncthreads();
+    if (wave) return;
+    for (int w = 1; w < LW; ++w) join_stats(st, sums[w], k);
+    if constexpr (TOP > 0) best = largest_of<TOP, 1>(LW, lane, [&](int i, int j) { return i < LW ? lists[i][j] : 0; });
+    finish(p, r, t, st, best, lane);
 }
 
 /* ---- host ------------------------------------------------------------------------------------------ */
 
-constexpr int VU = 4;
+constexpr int VU = 4, CHUNK = LT * VU * 4;
+constexpr int LEAST = 1;
+constexpr int SHARES = 1536;                  /* workgroups that the chip holds: six waves per SIMD */
 
 static LogPlan plan_of(const wsr_logprobs& p, void* ws, size_t* bytes) {
     LogPlan pl;
-    const int64_t chunks = (p.vocab + LT * VU * 4 - 1) / (LT * VU * 4);
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(chunks, 2048 / std::max<int64_t>(1, p.n_rows)));
-    pl.per = (int32_t)((chunks + want - 1) / want);
-    pl.parts = (int32_t)((chunks + pl.per - 1) / pl.per);
-    const size_t items = (size_t)p.n_rows * pl.parts, keys = (items * p.n_top * sizeof(key64) + 255) / 256 * 256;
-    if (bytes) *bytes = pl.parts == 1 ? 256 : keys + items * sizeof(LogStat);
+    pl.chunks = (uint32_t)((p.vocab + CHUNK - 1) / CHUNK);
+    pl.all = (uint32_t)std::min<int64_t>(p.n_rows * pl.chunks, UINT32_MAX);
+    pl.shares = (int32_t)std::max<uint32_t>(1, std::min<uint32_t>(SHARES, std::max<uint32_t>(std::min<uint32_t>(pl.all, 256), pl.all / LEAST)));
+    pl.each = pl.all / pl.shares, pl.rest = pl.all % pl.shares;
+    const size_t slots = 2 * (size_t)pl.shares, keys = (slots * p.n_top * sizeof(key64) + 255) / 256 * 256;
+    if (bytes) *bytes = keys + slots * sizeof(LogStat);
     pl.keys = static_cast<key64*>(ws);
     pl.stats = reinterpret_cast<LogStat*>(static_cast<char*>(ws) + keys);
     return pl;
@@ -315,15 +451,19 @@ size_t logprobs_workspace(const wsr_logprobs& p) {
     return n;
 }
 
+template <int TOP>
+static hipError_t launch_top(const wsr_logprobs& p, const LogPlan& pl, hipStream_t s) {
+    hipLaunchKernelGGL((k_logprobs<VU, TOP>), dim3((unsigned)pl.shares), dim3(LT), 0, s, p, pl);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || pl.chunks == 1 || (pl.rest == 0 && pl.each % pl.chunks == 0)) return e;
+    hipLaunchKernelGGL(k_logprobs_join<TOP>, dim3((unsigned)pl.shares - 1), dim3(LT), 0, s, p, pl);
+    return hipGetLastError();
+}
+
 hipError_t launch_logprobs(const wsr_logprobs& p, void* ws, hipStream_t s) {
     const LogPlan pl = plan_of(p, ws, nullptr);
-    const dim3 grid((unsigned)(p.n_rows * pl.parts)), threads(LT);
-    if (p.n_top) hipLaunchKernelGGL((k_logprobs<VU, true>), grid, threads, 0, s, p, pl);
-    else hipLaunchKernelGGL((k_logprobs<VU, false>), grid, threads, 0, s, p, pl);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || pl.parts == 1) return e;
-    hipLaunchKernelGGL(k_logprobs_join, dim3((unsigned)p.n_rows), dim3(WAVE), 0, s, p, pl);
-    return hipGetLastError();
+    return p.n_top == 0 ? launch_top<0>(p, pl, s) : p.n_top == 1 ? launch_top<1>(p, pl, s) : p.n_top <= 8 ? launch_top<8>(p, pl, s)
+           : p.n_top <= 32 ? launch_top<32>(p, pl, s) : launch_top<64>(p, pl, s);
 }
 
 }  // namespace wsr_serve

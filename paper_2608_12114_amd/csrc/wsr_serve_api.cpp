@@ -185,7 +185,8 @@ wsr_status wsr_paged_attention(const wsr_paged* p, void* ws, size_t ws_bytes, vo
 static wsr_status check_logprobs(const wsr_logprobs& p, const char* who) {
     if (p.n_rows < 0 || p.vocab < 1 || p.n_top < 0 || p.reserved) return fail(WSR_E_ARG, "%s: negative size or empty vocabulary", who);
     if (p.n_top > 64) return fail(WSR_E_SIZE, "%s: n_top=%d is above 64", who, p.n_top);
-    if (p.vocab > 1 << 24 || p.n_rows > 1 << 20) return fail(WSR_E_SIZE, "%s: vocab or n_rows too large", who);
+    if (p.vocab > 1 << 24 || p.n_rows > 1 << 20 || p.n_rows * p.vocab > (int64_t)1 << 40)
+        return fail(WSR_E_SIZE, "%s: vocab or n_rows too large", who);
     return WSR_OK;
 }
 

@@ -126,7 +126,8 @@ def _logprobs(**over):
 
 @pytest.mark.parametrize("over,st", [
     (dict(n_rows=-1), ARG), (dict(vocab=0), ARG), (dict(n_top=-1), ARG), (dict(n_top=65), SIZE), (dict(vocab=(1 << 24) + 1), SIZE),
-    (dict(n_rows=(1 << 20) + 1), SIZE), (dict(reserved=1), ARG), (dict(row_stride=-4), ALIGN), (dict(row_stride=6), ALIGN),
+    (dict(n_rows=(1 << 20) + 1), SIZE), (dict(n_rows=1 << 20, vocab=(1 << 20) + 1), SIZE), (dict(reserved=1), ARG),
+    (dict(row_stride=-4), ALIGN), (dict(row_stride=6), ALIGN),
     (dict(row_stride=1 << 62), SIZE), (dict(logits=A + 2), ALIGN), (dict(tokens=A + 1), ALIGN), (dict(temperature=A + 2), ALIGN),
     (dict(top=A + 2), ALIGN), (dict(logits=None), ARG), (dict(top=None), ARG), (dict(tokens=None), ARG),
     (dict(tokens=None, logp=None), ARG), (dict(n_rows=0), OK)])
