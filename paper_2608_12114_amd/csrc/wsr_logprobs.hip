@@ -14,6 +14,12 @@
  * over the wave.  The first chunk's threshold is the n-th largest of the lanes' maxima, which n logits reach.  A single
  * alternative is a lane's largest and needs none of this.
  *
+ * Bound by HBM and, less so, by the vector ALUs where rows are many: 2055 rows of 50257, 413 MB, 73 us without alternatives
+ * (5.6 TB/s; some fifteen instructions a logit), 79 with one, 93 with five, 801 rows of 128256 with 64 105 us.  Few rows are
+ * two launches' latency: one row of 128256 with five alternatives 12, 64 rows with none 13, with 20 22.  A bar of the
+ * workgroup's own for the alternatives, from what its waves have seen, took 23 of 128 us off 801 rows with 64, and 1.5 of 24
+ * off 64 with 20; the passing logits' registers skipped one by one 20 of 123 off 4001 rows of 25001 with five.
+ *
  * exp((l - m) / T) is taken as exp2((l - m) * (log2 e / T)): one rounding of the product, 2^-24 |l - m| / T relative.
  */
 #include <hip/hip_runtime.h>
@@ -203,13 +209,15 @@ struct Best {
         waiting += __builtin_popcountll(who);
     }
     /* ... and are merged, the last 64 at a time. */
-    __device__ __forceinline__ void drain(int lane) {
+    __device__ __forceinline__ bool drain(int lane) {
+        const bool any = waiting >= WAVE;
 #pragma unroll 1
         while (waiting >= WAVE) {
             waiting -= WAVE;
             wave_fence();
             merge(room[waiting + lane], lane);
         }
+        return any;
     }
     __device__ __forceinline__ void flush(int lane) {
         drain(lane);
@@ -245,6 +253,7 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_
     __shared__ key64 room[TOP > 1 ? LW : 1][ROOM];
     __shared__ key64 lists[2][LW][TOP > 0 ? TOP : 1];          /* by the parity of the part, so that one barrier a part is enough */
     __shared__ LogStat sums[2][LW];
+    __shared__ float quarter[2][LW];                            /* the n / 4-th largest logit that each wave has seen of the part */
     const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), n = (int)p.vocab;
     uint32_t at = pl.start(blockIdx.x);
     const uint32_t end = pl.start(blockIdx.x + 1);
@@ -259,7 +268,8 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_
         for (int u = 0; u < VU; ++u) {
             const int i = chunk * CHUNK + (u * LT + (int)threadIdx.x) * 4;
             if (i + 4 <= n) {
-                const f4_t q = *(const wsr_step::f4_any_t*)(from + i);
+                /* read once: 2055 rows of 50257 87.8 us without the hint, so 81 */
+                const f4_t q = __builtin_nontemporal_load((const wsr_step::f4_any_t*)(from + i));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) next[u][j] = q[j];
             } else {
@@ -272,6 +282,11 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_
     float t = temperature_of(p, r);
     load((const float*)row, c);
     Best<(TOP > 1 ? TOP : 2)> b;
+    const int fourth = (p.n_top + LW - 1) / LW - 1;
+    if constexpr (TOP > 1) {
+        if (lane == 0) quarter[0][wave] = quarter[1][wave] = NEG_INF;
+        __syncthreads();
+    }
     /* a part: chunks of one row */
 #pragma unroll 1
     for (int parity = 0; at < end; parity ^= 1) {
@@ -281,7 +296,10 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_
         const float mine = ranked ? no_nan(((const float*)row)[token]) : __builtin_inff();
         float m = NEG_INF, s = 0.f, e = 0.f, one = NEG_INF;
         int before = 0, one_at = 0x7fffffff;
-        if constexpr (TOP > 1) b.init(room[wave], p.n_top);
+        if constexpr (TOP > 1) {
+            b.init(room[wave], p.n_top);
+            if (lane == 0) quarter[parity ^ 1][wave] = NEG_INF;  /* for the next part: the last one's waves are all past it */
+        }
 #pragma unroll 1
         for (bool first = true; at < end && c < chunks; first = false, ++at, ++c) {
             float v[VU][4];
@@ -346,15 +364,24 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_
             }
             if constexpr (TOP > 1) {
                 if (first) {
-                    const float bar = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sorted<WAVE>(top, true, lane)), p.n_top - 1));
+                    const int order = __builtin_bit_cast(int, sorted<WAVE>(top, true, lane));
+                    const float bar = __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, p.n_top - 1));
                     if (bar > NEG_INF) b.raise(key_of(bar, -1));
+                    if (lane == 0) quarter[parity][wave] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, fourth));
+                    __syncthreads();
                 }
+                /* four waves that have seen n / 4 logits of at least this: no smaller one is among the workgroup's n */
+                float common = quarter[parity][0];
+#pragma unroll
+                for (int w = 1; w < LW; ++w) common = fminf(common, quarter[parity][w]);
+                if (common > b.bar) b.raise(key_of(common, -1));
                 if (__ballot(top >= b.bar && top > NEG_INF))
 #pragma unroll
                     for (int u = 0; u < VU; ++u) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) b.add(key_of(v[u][j], i0 + u * LT * 4 + j), v[u][j] > NEG_INF, lane);
-                        b.drain(lane);
+                        for (int j = 0; j < 4; ++j)
+                            if (__ballot(v[u][j] >= b.bar)) b.add(key_of(v[u][j], i0 + u * LT * 4 + j), v[u][j] > NEG_INF, lane);
+                        if (b.drain(lane) && lane == fourth) quarter[parity][wave] = logit_of(b.best);
                     }
             }
         }
@@ -429,7 +456,7 @@ __global__ __launch_bounds__(LT) void k_logprobs_join(wsr_logprobs p, LogPlan pl
 /* ---- host ------------------------------------------------------------------------------------------ */
 
 constexpr int VU = 4, CHUNK = LT * VU * 4;
-constexpr int LEAST = 1;
+constexpr int LEAST = 4;                      /* chunks of a share at least, once there are 256 of them */
 constexpr int SHARES = 1536;                  /* workgroups that the chip holds: six waves per SIMD */
 
 static LogPlan plan_of(const wsr_logprobs& p, void* ws, size_t* bytes) {
