@@ -39,11 +39,12 @@ constexpr float LAZY = 8.f;
 
 struct PagedPlan {
     int32_t rows;                             /* R, rows of a tile */
-    int32_t cuts;                             /* parts of all units together that are aimed at */
+    int32_t held;                             /* workgroups that the chip holds at a time */
+    int32_t slots;                            /* of parts */
     int32_t whole;                            /* no unit is cut */
     int32_t shift;                            /* division by page_size: (n * magic) >> shift for n < 2^31 */
     uint64_t magic;
-    float* part;                              /* [2 * cuts][R][head_dim + 4] */
+    float* part;                              /* [slots][R][head_dim + 4] */
 };
 
 /* ---- units and their parts -------------------------------------------------------------------------- */
@@ -69,16 +70,21 @@ __device__ __forceinline__ Seq seq_at(const wsr_paged& p, int R, int b) {
 /* Keys of a part, at most: as many as leave one part for each workgroup that the chip holds beside those that the units'
    ends cost, of LEAST or more.  Sums of lengths in fp32, which every wave rounds alike. */
 constexpr float LEAST = 256.f;
+constexpr float FILL = 0.125f, ROUNDS = 2.f, UP = 0.f, LEASTR = 128.f;
 struct Sums {
     float keys, units;
     __device__ __forceinline__ void add(const Seq& s, int N) { units += (float)s.tiles * N, keys += (float)s.tiles * N * s.len; }
 };
-__device__ __forceinline__ float part_of(const PagedPlan& pl, const Sums& s) {
-    return fmaxf(LEAST, s.keys / fmaxf((float)pl.cuts - s.units, (float)pl.cuts * 0.25f));
+struct Cut {
+    float part, up;                           /* keys of a part; what is added before the number of parts is rounded down */
+};
+__device__ __forceinline__ Cut cut_of(const PagedPlan& pl, const Sums& s) {
+    const float held = (float)pl.held, least = LEAST + LEASTR * (pl.rows / 16 - 1);
+    return s.units <= held * FILL ? Cut{fmaxf(least, s.keys / (held - s.units)), 0.999f} : Cut{fmaxf(least, s.keys / (held * ROUNDS)), UP};
 }
 /* Parts of each of a sequence's units. */
-__device__ __forceinline__ int parts_of(const Seq& s, float part) {
-    return (int)fminf(fmaxf(ceilf((float)s.len / part), 1.f), 65536.f);
+__device__ __forceinline__ int parts_of(const Seq& s, Cut cut) {
+    return (int)fminf(fmaxf(floorf((float)s.len / cut.part + cut.up), 1.f), 65536.f);
 }
 
 /* The lanes' sums of themselves and those below: inside 16-lane rows, then the rows' last lanes handed on. */
@@ -102,19 +108,19 @@ __device__ __forceinline__ bool find(const wsr_paged& p, const PagedPlan& pl, in
     const int lane = threadIdx.x % WAVE, N = p.n_kv_heads;
     Seq s{};
     if (lane < p.n_seqs) s = seq_at(p, pl.rows, lane);
-    float part = 0.f;
+    Cut cut{1.f, 0.f};
     if (!pl.whole) {
         Sums sums{0.f, 0.f};
         sums.add(s, N);
         for (int b = lane + WAVE; b < p.n_seqs; b += WAVE) sums.add(seq_at(p, pl.rows, b), N);
         sums.keys = wsr::wave_sum(sums.keys), sums.units = wsr::wave_sum(sums.units);
-        part = part_of(pl, sums);
+        cut = cut_of(pl, sums);
     }
     int items = 0, slots = 0;                 /* of the sequences before b0 */
     for (int b0 = 0; b0 < p.n_seqs; b0 += WAVE) {
         const int b = b0 + lane;
         if (b0) s = b < p.n_seqs ? seq_at(p, pl.rows, b) : Seq{};
-        const int parts = pl.whole ? 1 : parts_of(s, part), all = s.tiles * N * parts;
+        const int parts = pl.whole ? 1 : parts_of(s, cut), all = s.tiles * N * parts;
         const int to = scan32(all), slot_to = pl.whole ? 0 : scan32(parts > 1 ? all : 0);
         const uint64_t here = __ballot(by_seq ? b == item : items + to > item);
         if (here) {
@@ -341,8 +347,11 @@ __device__ __forceinline__ int opaque(int lane) {
     return lane;
 }
 
+/* Waves per SIMD that the registers of a form allow. */
+constexpr int waves_of(int D, int RT) { return D == 256 ? 1 : RT == 4 ? D == 64 ? 2 : 1 : RT == 2 ? D == 64 ? 3 : 2 : D == 64 ? 4 : 3; }
+
 template <int FMT, int D, int RT, int NW, bool ONCE>     /* NW: waves */
-__global__ __launch_bounds__(NW * WAVE) __attribute__((amdgpu_waves_per_eu(D == 256 ? 1 : D == 128 ? 3 : 4))) void k_paged(wsr_paged p, PagedPlan pl) {
+__global__ __launch_bounds__(NW * WAVE) __attribute__((amdgpu_waves_per_eu(waves_of(D, RT)))) void k_paged(wsr_paged p, PagedPlan pl) {
     typedef Walk<FMT, D, RT, ONCE> W;
     constexpr int R = W::R, STEP = KT * NW;
     __shared__ u32x4 lds_room[NW * W::ROOM / 16];
@@ -463,7 +472,7 @@ __global__ __launch_bounds__(NW * WAVE) __attribute__((amdgpu_waves_per_eu(D == 
             if (p.lse && wave == 0 && g == 0) p.lse[(int64_t)tok * p.n_heads + qh] = lse_of(m, l, p.scale);
         } else {
             const int slot = at_place.slot + at_place.at;
-            if (slot >= 2 * pl.cuts) continue;
+            if (slot >= pl.slots) continue;
             float* to = pl.part + ((int64_t)slot * R + row - row0) * (D + 4);
 #pragma unroll
             for (int i = 0; i < PER; ++i) *(f4_t*)(to + 16 * (wave + NW * i) + 4 * g) = sum[i];
@@ -489,7 +498,7 @@ __global__ __launch_bounds__(JT) void k_paged_join(wsr_paged p, PagedPlan pl) {
     if (b < 0 || !find(p, pl, b, true, o_place) || o_place.parts == 1) return;
     const int parts = o_place.parts, row = (tok - o_place.s.t0) * G + qh % G;
     const int slot0 = o_place.slot + (row / R * p.n_kv_heads + qh / G) * parts;
-    if (slot0 < 0 || slot0 + parts > 2 * pl.cuts) return;
+    if (slot0 < 0 || slot0 + parts > pl.slots) return;
     const float* from = pl.part + ((int64_t)slot0 * R + row % R) * (D + 4);
     const int64_t step = (int64_t)R * (D + 4);
     const float c = p.scale * LOG2E;
@@ -555,12 +564,19 @@ __global__ __launch_bounds__(JT) void k_paged_join(wsr_paged p, PagedPlan pl) {
 
 constexpr int WHOLE = 512;
 constexpr int FEW = 2048;
-constexpr float OVER = 1.f;
+
+/* Tiles of 16 rows of a workgroup: as many as a sequence's rows fill, on average. */
+static int row_tiles(const wsr_paged& p) {
+    const int64_t rows = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads);
+    return rows <= 16 * (int64_t)p.n_seqs ? 1 : rows <= 32 * (int64_t)p.n_seqs || p.head_dim == 256 ? 2 : 4;
+}
 
 static PagedPlan paged_plan(const wsr_paged& p) {
     PagedPlan pl{};
-    pl.rows = 16;
-    pl.cuts = (int)(OVER * (p.head_dim == 256 ? 256 : p.head_dim == 128 ? 768 : 1024));
+    const int rt = row_tiles(p);
+    pl.rows = 16 * rt;
+    pl.held = 256 * waves_of(p.head_dim, rt);
+    pl.slots = 4 * pl.held;
     pl.whole = p.max_len <= WHOLE;
     /* n / d = (n * M) >> (31 + s), 2^s >= d, M = 2^(31 + s) / d + 1, for n < 2^31: M d is over 2^(31 + s) by at most d */
     int s = 0;
@@ -572,7 +588,7 @@ static PagedPlan paged_plan(const wsr_paged& p) {
 
 size_t paged_workspace(const wsr_paged& p) {
     const PagedPlan pl = paged_plan(p);
-    return pl.whole ? 256 : (size_t)2 * pl.cuts * pl.rows * (p.head_dim + 4) * sizeof(float);
+    return pl.whole ? 256 : (size_t)pl.slots * pl.rows * (p.head_dim + 4) * sizeof(float);
 }
 
 /* Units of a call, at most. */
@@ -583,7 +599,7 @@ static int64_t most_units(const wsr_paged& p, const PagedPlan& pl) {
 
 template <int FMT, int D, int RT, int NW, bool ONCE>
 static hipError_t launch_form(const wsr_paged& p, const PagedPlan& pl, hipStream_t s) {
-    const int64_t blocks = most_units(p, pl) + (pl.whole ? 0 : pl.cuts + 16);
+    const int64_t blocks = most_units(p, pl) + (pl.whole ? 0 : pl.slots);
     hipLaunchKernelGGL((k_paged<FMT, D, RT, NW, ONCE>), dim3((unsigned)blocks), dim3(NW * WAVE), 0, s, p, pl);
     return hipGetLastError();
 }
@@ -591,7 +607,10 @@ static hipError_t launch_form(const wsr_paged& p, const PagedPlan& pl, hipStream
 template <int FMT, int D>
 static hipError_t launch_dim(const wsr_paged& p, const PagedPlan& pl, hipStream_t s) {
     const bool once = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads) <= (int64_t)pl.rows * p.n_seqs;
-    hipError_t e = once ? launch_form<FMT, D, 1, 4, true>(p, pl, s) : launch_form<FMT, D, 1, 4, false>(p, pl, s);
+    hipError_t e = hipSuccess;
+    if (pl.rows == 16) e = launch_form<FMT, D, 1, 4, true>(p, pl, s);
+    else if (pl.rows == 32) e = once ? launch_form<FMT, D, 2, 4, true>(p, pl, s) : launch_form<FMT, D, 2, 4, false>(p, pl, s);
+    else if constexpr (D < 256) e = once ? launch_form<FMT, D, 4, 4, true>(p, pl, s) : launch_form<FMT, D, 4, 4, false>(p, pl, s);
     if (pl.whole) return e;
     if (e != hipSuccess) return e;
     const int64_t rows = (int64_t)p.n_tokens * p.n_heads;       /* at most 2^26: one launch */
