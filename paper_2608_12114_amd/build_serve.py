@@ -7,7 +7,7 @@ import os
 from . import build as wb
 
 LIB_PATH = os.path.join(wb.PKG, "libwsr_serve.so")
-KERNEL_FILES = ("wsr_append.hip", "wsr_paged.hip", "wsr_logprobs.hip")
+KERNEL_FILES = ("wsr_append.hip", "wsr_paged.hip", "wsr_paged_rows.hip", "wsr_logprobs.hip")
 
 
 def _compile_api() -> str:

@@ -21,7 +21,7 @@
 
 #include <algorithm>
 
-#include "wsr_serve_device.h"
+#include "wsr_paged.h"
 
 namespace wsr_serve {
 
@@ -36,108 +36,6 @@ typedef __attribute__((address_space(3))) u32x4 l_u32x4;
 /* The running maximum is only moved when a row's scores pass it by 2^LAZY: until then its probabilities are taken
    against the old one (at most 2^LAZY, exact after the division by their sum). */
 constexpr float LAZY = 8.f;
-
-struct PagedPlan {
-    int32_t rows;                             /* R, rows of a tile */
-    int32_t held;                             /* workgroups that the chip holds at a time */
-    int32_t slots;                            /* of parts */
-    int32_t whole;                            /* no unit is cut */
-    int32_t shift;                            /* division by page_size: (n * magic) >> shift for n < 2^31 */
-    uint64_t magic;
-    float* part;                              /* [slots][R][head_dim + 4] */
-};
-
-/* ---- units and their parts -------------------------------------------------------------------------- */
-
-struct Seq {
-    int32_t t0, n, len;                       /* first token, tokens, keys */
-    int32_t rows, tiles;
-};
-__device__ __forceinline__ Seq seq_at(const wsr_paged& p, int R, int b) {
-    Seq s;
-    int next;
-    if (p.starts) {
-        s.t0 = min(max(p.starts[b], 0), p.n_tokens);
-        next = min(max(p.starts[b + 1], s.t0), p.n_tokens);
-    } else s.t0 = b, next = b + 1;
-    s.n = next - s.t0;
-    s.len = (int)min(max((int64_t)p.lens[b], (int64_t)0), p.max_len);
-    s.rows = s.n * (p.n_heads / p.n_kv_heads);
-    s.tiles = (s.rows + R - 1) / R;
-    return s;
-}
-
-/* Keys of a part, at most: as many as leave one part for each workgroup that the chip holds beside those that the units'
-   ends cost, of LEAST or more.  Sums of lengths in fp32, which every wave rounds alike. */
-constexpr float LEAST = 256.f;
-constexpr float FILL = 0.125f, ROUNDS = 2.f, UP = 0.f, LEASTR = 128.f;
-struct Sums {
-    float keys, units;
-    __device__ __forceinline__ void add(const Seq& s, int N) { units += (float)s.tiles * N, keys += (float)s.tiles * N * s.len; }
-};
-struct Cut {
-    float part, up;                           /* keys of a part; what is added before the number of parts is rounded down */
-};
-__device__ __forceinline__ Cut cut_of(const PagedPlan& pl, const Sums& s) {
-    const float held = (float)pl.held, least = LEAST + LEASTR * (pl.rows / 16 - 1);
-    return s.units <= held * FILL ? Cut{fmaxf(least, s.keys / (held - s.units)), 0.999f} : Cut{fmaxf(least, s.keys / (held * ROUNDS)), UP};
-}
-/* Parts of each of a sequence's units. */
-__device__ __forceinline__ int parts_of(const Seq& s, Cut cut) {
-    return (int)fminf(fmaxf(floorf((float)s.len / cut.part + cut.up), 1.f), 65536.f);
-}
-
-/* The lanes' sums of themselves and those below: inside 16-lane rows, then the rows' last lanes handed on. */
-__device__ __forceinline__ int scan32(int v) {
-    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     /* from one lane below, two, four, eight */
-    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     /* lane 15 of a row to the next, of rows 1 and 3 */
-    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);     /* lane 31 to rows 2 and 3 */
-    return v;
-}
-
-struct Place {
-    Seq s;
-    int seq, at, parts, slot;                 /* at: item of the sequence; slot: of the sequence's first part */
-};
-/* Item `item` of the call, or (by_seq) the first of sequence `item`: its sequence, how that is cut and where its parts lie.
-   False where there is no such item. */
-__device__ __forceinline__ bool find(const wsr_paged& p, const PagedPlan& pl, int item, bool by_seq, Place& o) {
-    const int lane = threadIdx.x % WAVE, N = p.n_kv_heads;
-    Seq s{};
-    if (lane < p.n_seqs) s = seq_at(p, pl.rows, lane);
-    Cut cut{1.f, 0.f};
-    if (!pl.whole) {
-        Sums sums{0.f, 0.f};
-        sums.add(s, N);
-        for (int b = lane + WAVE; b < p.n_seqs; b += WAVE) sums.add(seq_at(p, pl.rows, b), N);
-        sums.keys = wsr::wave_sum(sums.keys), sums.units = wsr::wave_sum(sums.units);
-        cut = cut_of(pl, sums);
-    }
-    int items = 0, slots = 0;                 /* of the sequences before b0 */
-    for (int b0 = 0; b0 < p.n_seqs; b0 += WAVE) {
-        const int b = b0 + lane;
-        if (b0) s = b < p.n_seqs ? seq_at(p, pl.rows, b) : Seq{};
-        const int parts = pl.whole ? 1 : parts_of(s, cut), all = s.tiles * N * parts;
-        const int to = scan32(all), slot_to = pl.whole ? 0 : scan32(parts > 1 ? all : 0);
-        const uint64_t here = __ballot(by_seq ? b == item : items + to > item);
-        if (here) {
-            const int w = __builtin_ctzll(here);
-            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, w); };
-            o.s = Seq{of(s.t0), of(s.n), of(s.len), of(s.rows), of(s.tiles)};
-            o.seq = b0 + w;
-            o.parts = of(parts);
-            o.at = item - (items + of(to) - of(all));
-            o.slot = slots + of(slot_to) - (o.parts > 1 ? of(all) : 0);
-            return true;
-        }
-        items += __builtin_amdgcn_readlane(to, WAVE - 1);
-        slots += __builtin_amdgcn_readlane(slot_to, WAVE - 1);
-    }
-    return false;
-}
 
 /* ---- a wave's walk ----------------------------------------------------------------------------------- */
 
@@ -336,19 +234,8 @@ struct Walk {
     }
 };
 
-/* log of a row's sum l against its maximum m: -inf where it saw no key, NaN where a score was. */
-__device__ __forceinline__ float lse_of(float m, float l, float scale) { return l == 0.f ? NEG_INF : m * scale + logf(l); }
-__device__ __forceinline__ float inverse_of(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; }
-
-/* The lane's number anew: what follows from it is computed again, a few instructions, where it would hold registers through
-   the loop. */
-__device__ __forceinline__ int opaque(int lane) {
-    asm volatile("" : "+v"(lane));
-    return lane;
-}
-
 /* Waves per SIMD that the registers of a form allow. */
-constexpr int waves_of(int D, int RT) { return D == 256 ? 1 : RT == 4 ? D == 64 ? 2 : 1 : RT == 2 ? D == 64 ? 3 : 2 : D == 64 ? 4 : 3; }
+constexpr int waves_of(int D, int RT) { return D == 256 ? 1 : RT == 2 ? D == 64 ? 3 : 2 : D == 64 ? 4 : 3; }
 
 template <int FMT, int D, int RT, int NW, bool ONCE>     /* NW: waves */
 __global__ __launch_bounds__(NW * WAVE) __attribute__((amdgpu_waves_per_eu(waves_of(D, RT)))) void k_paged(wsr_paged p, PagedPlan pl) {
@@ -565,17 +452,16 @@ __global__ __launch_bounds__(JT) void k_paged_join(wsr_paged p, PagedPlan pl) {
 constexpr int WHOLE = 512;
 constexpr int FEW = 2048;
 
-/* Tiles of 16 rows of a workgroup: as many as a sequence's rows fill, on average. */
-static int row_tiles(const wsr_paged& p) {
-    const int64_t rows = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads);
-    return rows <= 16 * (int64_t)p.n_seqs ? 1 : rows <= 32 * (int64_t)p.n_seqs || p.head_dim == 256 ? 2 : 4;
+/* Rows of a tile: as many as a sequence's fill, on average. */
+static int tile_rows(const wsr_paged& p) {
+    const int64_t rows = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads), n = p.n_seqs;
+    return rows <= 16 * n ? 16 : rows <= 32 * n || p.head_dim == 256 ? 32 : rows <= 64 * n ? 64 : 128;
 }
 
 static PagedPlan paged_plan(const wsr_paged& p) {
     PagedPlan pl{};
-    const int rt = row_tiles(p);
-    pl.rows = 16 * rt;
-    pl.held = 256 * waves_of(p.head_dim, rt);
+    pl.rows = tile_rows(p);
+    pl.held = 256 * (pl.rows > 32 ? 2 : waves_of(p.head_dim, pl.rows / 16));
     pl.slots = 4 * pl.held;
     pl.whole = p.max_len <= WHOLE;
     /* n / d = (n * M) >> (31 + s), 2^s >= d, M = 2^(31 + s) / d + 1, for n < 2^31: M d is over 2^(31 + s) by at most d */
@@ -597,22 +483,21 @@ static int64_t most_units(const wsr_paged& p, const PagedPlan& pl) {
     return p.n_kv_heads * (rows / pl.rows + std::min(p.n_seqs, p.n_tokens));
 }
 
-template <int FMT, int D, int RT, int NW, bool ONCE>
-static hipError_t launch_form(const wsr_paged& p, const PagedPlan& pl, hipStream_t s) {
-    const int64_t blocks = most_units(p, pl) + (pl.whole ? 0 : pl.slots);
-    hipLaunchKernelGGL((k_paged<FMT, D, RT, NW, ONCE>), dim3((unsigned)blocks), dim3(NW * WAVE), 0, s, p, pl);
-    return hipGetLastError();
-}
-
 template <int FMT, int D>
 static hipError_t launch_dim(const wsr_paged& p, const PagedPlan& pl, hipStream_t s) {
+    const int64_t blocks = most_units(p, pl) + (pl.whole ? 0 : pl.slots);
+    const dim3 grid((unsigned)blocks), threads(4 * WAVE);
     const bool once = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads) <= (int64_t)pl.rows * p.n_seqs;
-    hipError_t e = hipSuccess;
-    if (pl.rows == 16) e = launch_form<FMT, D, 1, 4, true>(p, pl, s);
-    else if (pl.rows == 32) e = once ? launch_form<FMT, D, 2, 4, true>(p, pl, s) : launch_form<FMT, D, 2, 4, false>(p, pl, s);
-    else if constexpr (D < 256) e = once ? launch_form<FMT, D, 4, 4, true>(p, pl, s) : launch_form<FMT, D, 4, 4, false>(p, pl, s);
-    if (pl.whole) return e;
-    if (e != hipSuccess) return e;
+    hipError_t e;
+    if (pl.rows > 32) {
+        e = launch_paged_rows(p, pl, pl.rows / 32, once, blocks, s);
+    } else {
+        if (pl.rows == 16) hipLaunchKernelGGL((k_paged<FMT, D, 1, 4, true>), grid, threads, 0, s, p, pl);
+        else if (once) hipLaunchKernelGGL((k_paged<FMT, D, 2, 4, true>), grid, threads, 0, s, p, pl);
+        else hipLaunchKernelGGL((k_paged<FMT, D, 2, 4, false>), grid, threads, 0, s, p, pl);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess || pl.whole) return e;
     const int64_t rows = (int64_t)p.n_tokens * p.n_heads;       /* at most 2^26: one launch */
     if (rows <= FEW) hipLaunchKernelGGL((k_paged_join<FMT, D, JW>), dim3((unsigned)rows), dim3(JT), 0, s, p, pl);
     else hipLaunchKernelGGL((k_paged_join<FMT, D, 1>), dim3((unsigned)((rows + JW - 1) / JW)), dim3(JT), 0, s, p, pl);
