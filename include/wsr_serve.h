@@ -98,8 +98,8 @@ wsr_status wsr_append_qkv(const wsr_qkv* p, void* stream);
    statistics and sums are fp32, probabilities are rounded to `fmt` for the product with the values, out once to `fmt`.
    Rows of q that belong to no sequence (before starts[0], from starts[n_seqs] on) keep what out and lse held.
    starts: device int32 [n_seqs + 1], not decreasing; lens: device int32 [n_seqs], clamped to [0, max_len];
-   max_len <= max_pages * page_size.  n_tokens and n_seqs at most 2^20, n_heads at most 4096 and 512 times
-   n_kv_heads, tokens times heads at most 2^26.  head_dim 64, 128 or 256; every pointer 16-byte aligned and every stride a
+   max_len <= max_pages * page_size.  n_tokens and n_seqs at most 2^20, n_heads at most 4096, tokens times
+   heads at most 2^25; n_kv_heads * (n_seqs + a key head's rows / 16) past 2^23 may be refused.  head_dim 64, 128 or 256; every pointer 16-byte aligned and every stride a
    multiple of 16 (of 4 for table, starts, lens and lse); lse (n_tokens, n_heads) or null.  ws:
    wsr_paged_workspace_bytes(), 256-byte aligned. */
 typedef struct wsr_paged {

@@ -78,37 +78,53 @@ struct Place {
    False where there is no such item. */
 __device__ __forceinline__ bool find(const wsr_paged& p, const PagedPlan& pl, int item, bool by_seq, Place& o) {
     const int lane = threadIdx.x % WAVE, N = p.n_kv_heads;
-    Seq s{};
-    if (lane < p.n_seqs) s = seq_at(p, pl.rows, lane);
+    /* sequence b of those from lo on, nothing from lo + n on; loads without a branch, so that several are on their way at once */
+    auto seq_in = [&](int b, int lo, int n) {
+        Seq s = seq_at(p, pl.rows, min(lo + b, p.n_seqs - 1));
+        if (b >= n) s.rows = s.tiles = s.n = s.len = 0;
+        return s;
+    };
+    Seq s = seq_in(lane, 0, p.n_seqs);
     Cut cut{1.f, 0.f};
     if (!pl.whole) {
         Sums sums{0.f, 0.f};
         sums.add(s, N);
-        for (int b = lane + WAVE; b < p.n_seqs; b += WAVE) sums.add(seq_at(p, pl.rows, b), N);
+#pragma unroll 4
+        for (int b = WAVE; b < p.n_seqs; b += WAVE) sums.add(seq_in(b + lane, 0, p.n_seqs), N);
         sums.keys = wsr::wave_sum(sums.keys), sums.units = wsr::wave_sum(sums.units);
         cut = cut_of(pl, sums);
     }
-    int items = 0, slots = 0;                 /* of the sequences before b0 */
-    for (int b0 = 0; b0 < p.n_seqs; b0 += WAVE) {
-        const int b = b0 + lane;
-        if (b0) s = b < p.n_seqs ? seq_at(p, pl.rows, b) : Seq{};
-        const int parts = pl.whole ? 1 : parts_of(s, cut), all = s.tiles * N * parts;
-        const int to = scan32(all), slot_to = pl.whole ? 0 : scan32(parts > 1 ? all : 0);
-        const uint64_t here = __ballot(by_seq ? b == item : items + to > item);
-        if (here) {
-            const int w = __builtin_ctzll(here);
-            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, w); };
+    int lo = 0, n = p.n_seqs;                 /* the sequences left, and items and slots of those before them */
+    int items = 0, slots = 0;
+    while (true) {                            /* to a 64th of them at a time */
+        const int per = (n + WAVE - 1) / WAVE;
+        int parts = 1, all = 0, cuts = 0;
+        auto count = [&]() __attribute__((always_inline)) {
+            if (!pl.whole) parts = parts_of(s, cut);
+            const int mine = s.tiles * N * parts;
+            all += mine, cuts += parts > 1 ? mine : 0;
+        };
+        if (per == 1) {
+            if (p.n_seqs > WAVE) s = seq_in(lane, lo, n);
+            count();
+        } else {
+            const int end = min(lane * per + per, n);
+#pragma unroll 4
+            for (int i = 0; i < per; ++i) s = seq_in(lane * per + i, lo, end), count();
+        }
+        const int to = scan32(all), cuts_to = pl.whole ? 0 : scan32(cuts);
+        const uint64_t here = __ballot(by_seq ? (uint32_t)(item - lo - lane * per) < (uint32_t)per : items + to > item);
+        if (!here) return false;
+        const int w = __builtin_ctzll(here);
+        auto of = [&](int v) { return __builtin_amdgcn_readlane(v, w); };
+        items += of(to) - of(all), slots += of(cuts_to) - of(cuts);
+        if (per == 1) {
             o.s = Seq{of(s.t0), of(s.n), of(s.len), of(s.rows), of(s.tiles)};
-            o.seq = b0 + w;
-            o.parts = of(parts);
-            o.at = item - (items + of(to) - of(all));
-            o.slot = slots + of(slot_to) - (o.parts > 1 ? of(all) : 0);
+            o.seq = lo + w, o.parts = of(parts), o.at = item - items, o.slot = slots;
             return true;
         }
-        items += __builtin_amdgcn_readlane(to, WAVE - 1);
-        slots += __builtin_amdgcn_readlane(slot_to, WAVE - 1);
+        lo += w * per, n = min(per, n - w * per);
     }
-    return false;
 }
 
 /* log of a row's sum l against its maximum m: -inf where it saw no key, NaN where a score was. */

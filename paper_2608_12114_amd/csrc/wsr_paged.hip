@@ -449,7 +449,7 @@ __global__ __launch_bounds__(JT) void k_paged_join(wsr_paged p, PagedPlan pl) {
 
 /* ---- host ------------------------------------------------------------------------------------------ */
 
-constexpr int WHOLE = 512;
+constexpr int WIDE = 256;
 constexpr int FEW = 2048;
 
 /* Rows of a tile: as many as a sequence's fill, on average. */
@@ -463,7 +463,7 @@ static PagedPlan paged_plan(const wsr_paged& p) {
     pl.rows = tile_rows(p);
     pl.held = 256 * (pl.rows > 32 ? 2 : waves_of(p.head_dim, pl.rows / 16));
     pl.slots = 4 * pl.held;
-    pl.whole = p.max_len <= WHOLE;
+    pl.whole = p.max_len <= ((int64_t)p.n_kv_heads * std::min(p.n_seqs, p.n_tokens) < WIDE ? 768 : 1536);
     /* n / d = (n * M) >> (31 + s), 2^s >= d, M = 2^(31 + s) / d + 1, for n < 2^31: M d is over 2^(31 + s) by at most d */
     int s = 0;
     while ((int64_t)1 << s < p.cache.page_size) ++s;
@@ -483,22 +483,28 @@ static int64_t most_units(const wsr_paged& p, const PagedPlan& pl) {
     return p.n_kv_heads * (rows / pl.rows + std::min(p.n_seqs, p.n_tokens));
 }
 
+/* Workgroups of the first launch. */
+static int64_t paged_blocks(const wsr_paged& p, const PagedPlan& pl) { return most_units(p, pl) + (pl.whole ? 0 : pl.slots); }
+bool paged_fits(const wsr_paged& p) { return paged_blocks(p, paged_plan(p)) <= most_blocks(4 * WAVE); }
+
 template <int FMT, int D>
 static hipError_t launch_dim(const wsr_paged& p, const PagedPlan& pl, hipStream_t s) {
-    const int64_t blocks = most_units(p, pl) + (pl.whole ? 0 : pl.slots);
+    const int64_t blocks = paged_blocks(p, pl);
     const dim3 grid((unsigned)blocks), threads(4 * WAVE);
     const bool once = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads) <= (int64_t)pl.rows * p.n_seqs;
     hipError_t e;
     if (pl.rows > 32) {
         e = launch_paged_rows(p, pl, pl.rows / 32, once, blocks, s);
     } else {
-        if (pl.rows == 16) hipLaunchKernelGGL((k_paged<FMT, D, 1, 4, true>), grid, threads, 0, s, p, pl);
+        if (pl.rows == 16 && pl.whole && D < 256 && (int64_t)p.n_kv_heads * p.n_seqs < WIDE)
+            hipLaunchKernelGGL((k_paged<FMT, D, 1, (D < 256 ? 12 : 4), true>), grid, dim3(12 * WAVE), 0, s, p, pl);
+        else if (pl.rows == 16) hipLaunchKernelGGL((k_paged<FMT, D, 1, 4, true>), grid, threads, 0, s, p, pl);
         else if (once) hipLaunchKernelGGL((k_paged<FMT, D, 2, 4, true>), grid, threads, 0, s, p, pl);
         else hipLaunchKernelGGL((k_paged<FMT, D, 2, 4, false>), grid, threads, 0, s, p, pl);
         e = hipGetLastError();
     }
     if (e != hipSuccess || pl.whole) return e;
-    const int64_t rows = (int64_t)p.n_tokens * p.n_heads;       /* at most 2^26: one launch */
+    const int64_t rows = (int64_t)p.n_tokens * p.n_heads;       /* at most 2^25: one launch */
     if (rows <= FEW) hipLaunchKernelGGL((k_paged_join<FMT, D, JW>), dim3((unsigned)rows), dim3(JT), 0, s, p, pl);
     else hipLaunchKernelGGL((k_paged_join<FMT, D, 1>), dim3((unsigned)((rows + JW - 1) / JW)), dim3(JT), 0, s, p, pl);
     return hipGetLastError();

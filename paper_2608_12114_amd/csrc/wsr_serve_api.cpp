@@ -145,15 +145,14 @@ static wsr_status check_paged(const wsr_paged& p, const char* who) {
         return fail(WSR_E_ARG, "%s: n_heads=%d must be a multiple of n_kv_heads=%d, at most 4096", who, p.n_heads, p.n_kv_heads);
     if (p.n_seqs < 0 || p.n_tokens < 0 || p.max_len < 0 || p.reserved) return fail(WSR_E_ARG, "%s: negative size", who);
     if (p.n_tokens > 1 << 20 || p.n_seqs > 1 << 20) return fail(WSR_E_SIZE, "%s: too many tokens or sequences", who);
-    /* the line of work, rows / 16 tiles times keys times G, is counted in 64 bits */
-    if (p.n_heads / p.n_kv_heads > 512) return fail(WSR_E_SIZE, "%s: more than 512 query heads of a key head", who);
-    if ((int64_t)p.n_tokens * p.n_heads > 1 << 26) return fail(WSR_E_SIZE, "%s: tokens times heads above 2^26", who);
+    if ((int64_t)p.n_tokens * p.n_heads > 1 << 25) return fail(WSR_E_SIZE, "%s: tokens times heads above 2^25", who);
     if (!(p.scale > 0.f) || !std::isfinite(p.scale)) return fail(WSR_E_ARG, "%s: scale must be positive and finite", who);
     if (!p.starts && p.n_tokens != p.n_seqs) return fail(WSR_E_ARG, "%s: without starts each sequence has one token", who);
     if (p.n_seqs == 0 && p.n_tokens > 0) return fail(WSR_E_ARG, "%s: tokens of no sequence", who);
     WSR_TRY(check_pages(p.cache, p.n_seqs, p.n_kv_heads, who));
     if (p.max_len > (int64_t)p.cache.max_pages * p.cache.page_size)
         return fail(WSR_E_SIZE, "%s: max_len=%lld is more than max_pages hold", who, (long long)p.max_len);
+    if (!wsr_serve::paged_fits(p)) return fail(WSR_E_SIZE, "%s: too many sequences and key heads for one launch", who);
     return WSR_OK;
 }
 

@@ -13,6 +13,7 @@ namespace wsr_serve {
 
 hipError_t launch_append(const wsr_qkv& p, hipStream_t s);
 
+bool paged_fits(const wsr_paged& p);           /* one launch holds the call's units */
 size_t paged_workspace(const wsr_paged& p);
 hipError_t launch_paged(const wsr_paged& p, void* ws, hipStream_t s);
 

@@ -99,8 +99,8 @@ def _paged(cache=None, **over):
 
 @pytest.mark.parametrize("over,st", [
     (dict(fmt=0), ARG), (dict(head_dim=96), SIZE), (dict(n_heads=5), ARG), (dict(n_kv_heads=0), ARG), (dict(n_heads=1), ARG),
-    (dict(n_heads=1026, n_kv_heads=2), SIZE), (dict(n_seqs=-1), ARG), (dict(n_tokens=-1), ARG), (dict(max_len=-1), ARG),
-    (dict(max_len=65), SIZE), (dict(n_tokens=(1 << 20) + 1), SIZE), (dict(n_tokens=1 << 20, n_heads=128), SIZE), (dict(scale=0.0), ARG),
+    (dict(n_heads=8192), ARG), (dict(n_seqs=-1), ARG), (dict(n_tokens=-1), ARG), (dict(max_len=-1), ARG),
+    (dict(max_len=65), SIZE), (dict(n_tokens=(1 << 20) + 1), SIZE), (dict(n_tokens=1 << 20, n_heads=64), SIZE), (dict(scale=0.0), ARG),
     (dict(scale=math.inf), ARG), (dict(scale=math.nan), ARG), (dict(starts=None), ARG), (dict(n_seqs=0), ARG), (dict(reserved=1), ARG),
     (dict(q=None), ARG), (dict(out=None), ARG), (dict(lens=None), ARG), (dict(q=A + 8), ALIGN), (dict(out=A + 4), ALIGN),
     (dict(lens=A + 2), ALIGN), (dict(starts=A + 1), ALIGN), (dict(lse=A + 2), ALIGN), (dict(q_tok_stride=8), ALIGN),
