@@ -81,7 +81,7 @@ typedef struct wsr_qkv {
     const float* freqs;
     const int32_t *axis_of, *positions;
     int64_t pos_axis_stride;
-    const int32_t *starts, *lens; /* device int32 [n_seqs + 1], not decreasing, and [n_seqs] */
+    const int32_t *starts, *lens; /* device int32 [n_seqs + 1], not decreasing, clamped to [0, n_tokens]; [n_seqs], from 0 */
     void* q_out;
     int64_t q_out_tok_stride, q_out_head_stride;
     wsr_pages cache;
@@ -97,7 +97,8 @@ wsr_status wsr_append_qkv(const wsr_qkv* p, void* stream);
    holes are never read into a result.  Query head h reads key head h / (n_heads / n_kv_heads).  Types `fmt`; scores, softmax
    statistics and sums are fp32, probabilities are rounded to `fmt` for the product with the values, out once to `fmt`.
    Rows of q that belong to no sequence (before starts[0], from starts[n_seqs] on) keep what out and lse held.
-   starts: device int32 [n_seqs + 1], not decreasing; lens: device int32 [n_seqs], clamped to [0, max_len];
+   starts: device int32 [n_seqs + 1], not decreasing, clamped to [0, n_tokens]; lens: device int32 [n_seqs], clamped to
+   [0, max_len];
    max_len <= max_pages * page_size.  n_tokens and n_seqs at most 2^20, n_heads at most 4096, tokens times
    heads at most 2^25; n_kv_heads * (n_seqs + a key head's rows / 16) past 2^23 may be refused.  head_dim 64, 128 or 256; every pointer 16-byte aligned and every stride a
    multiple of 16 (of 4 for table, starts, lens and lse); lse (n_tokens, n_heads) or null.  ws:

@@ -97,7 +97,7 @@ __global__ __launch_bounds__(PT) void k_append(wsr_qkv p, Steps st, int64_t firs
 
     const Belongs of = seq_of(p.starts, p.n_seqs, tok);
     if (of.seq < 0) return;
-    const int64_t place = (int64_t)max(p.lens[of.seq], 0) - of.end + tok;
+    const int64_t place = (int64_t)max(p.lens[of.seq], 0) - min(of.end, p.n_tokens) + tok;
     int page = 0, slot = 0;
     const bool stored = p.k && p.n_kv_heads > 0 && page_of(p.cache, of.seq, place, page, slot);
 

@@ -1,0 +1,91 @@
+"""wsr_paged_attention in each of its forms, on both sides of the choices between them: tiles of 16 to 128 rows, one launch and
+two, units cut into few and many parts, sequences found in one and several steps."""
+import pytest
+import torch
+
+import serve_util as su
+from gpu_util import needs_gpu
+from test_gpu_serve_paged import BF16, F16, INF, NAN, Case
+
+pytestmark = [pytest.mark.gpu, needs_gpu]
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("G,n", [(8, 1), (8, 3), (4, 8), (8, 7), (5, 13), (8, 40), (3, 101)])
+@pytest.mark.parametrize("room", [0, 2000])
+def test_tiles(D, G, n, room):
+    """8 to 320 rows of a sequence, with and without room for a second launch; a tile's last rows empty."""
+    c = Case([n, max(1, n // 2), n], [n + 700, n, n + 123], 2 * G, 2, D, F16, page=12, room=room, seed=n)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,n", [(8, 1), (8, 3), (8, 8), (4, 40)])
+def test_units_cut_into_parts(D, G, n):
+    """A long sequence beside short ones: parts of different numbers, some of them joined, others stored at once."""
+    c = Case([n] * 5, [n + 5000, n, n + 40, n + 1700, n + 2600], G, 1, D, BF16, page=33, seed=D)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("n,lens", [(1, 1500), (6, 900), (40, 1300), (64, 2500)])
+@pytest.mark.parametrize("page", [1, 19, 64])
+def test_holes_in_every_form(n, lens, page):
+    row = -(-(lens + n) // page)
+    holes = [((0, i), (-1, 1 << 30)[i % 2]) for i in range(row) if i * page % 256 < 100] + [((1, i), -7) for i in range(row)]
+    c = Case([n, n, n], [lens + n, 200 + n, n], 8, 2, 128, F16, page=page, holes=holes)
+    c.run()
+    c.check()
+    assert torch.isneginf(c.lse[n:2 * n]).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [3, 8, 40])
+@pytest.mark.parametrize("value", [INF, NAN])
+def test_broken_values_in_every_form(n, D, value):
+    """An infinity or NaN among the values of a place that only the later queries see."""
+    lens = 1400 + n
+    c = Case([n], [lens], 8, 1, D, F16, page=8)
+    place = lens - n // 2
+    c.v[int(c.table[0, place // 8]), place % 8, 0, 5] = value
+    c.run()
+    first = next(i for i in range(n) if place < lens - n + i + 1)
+    hit = torch.zeros_like(c.out, dtype=torch.bool)
+    hit[first:, :, 5] = True
+    assert (torch.isnan(c.out[hit]) if value != value else c.out[hit] == value).all()
+    c.v[int(c.table[0, place // 8]), place % 8, 0, 5] = 0.0
+    out, _, bound, _ = su.paged64(c.q, c.k, c.v, c.table, 8, c.starts, c.lens, c.max_len, c.scale)
+    assert ((c.out.double() - out).abs()[~hit] <= bound[~hit]).all()
+
+
+@pytest.mark.parametrize("n", [8, 40])
+def test_rows_without_keys_in_every_form(n):
+    """More queries than keys, and lengths of zero, among tiles that others fill."""
+    c = Case([n, n, 1, n], [n // 2, 0, 300, n + 900], 8, 1, 128, BF16, page=5, first=2, after=3)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("seqs", [64, 65, 300, 5000])
+@pytest.mark.parametrize("room", [0, 3000])
+def test_numbers_of_sequences(seqs, room):
+    counts = [1 + (b % 7 == 0) - (b % 5 == 0) for b in range(seqs)]
+    c = Case(counts, [n + (13 * b) % 37 for b, n in enumerate(counts)], 2, 1, 64, F16, page=8, room=room)
+    c.run()
+    c.check()
+
+
+def test_starts_are_clamped():
+    """What the device says past the rows of q is clamped to them."""
+    c = Case([2, 3], [40, 9], 4, 2, 64, F16)
+    c.dev_starts.copy_(torch.tensor([-5, 2, 1 << 30]))
+    c.run()
+    c.check()
+
+
+def test_one_sequence_beside_many_key_heads():
+    """Units enough for one launch without a cut where sequences are few."""
+    c = Case([1, 1], [1400, 1000], 256, 256, 64, BF16)
+    c.run()
+    c.check()
