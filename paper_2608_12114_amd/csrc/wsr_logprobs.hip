@@ -5,8 +5,9 @@
  *   entropy = log s + sum p (m - l) / T
  *
  * One read of a row: every lane keeps a maximum of its own and the two sums against it, and the wave how many logits come
- * before the given token's.  All rows' chunks lie on one line of which every workgroup takes an equal share, so that any
- * number of rows fills the chip; rows that lie in several shares are joined in a second launch.
+ * before the given token's.  A row is a workgroup's, or, where rows are few, several parts' that a second launch joins.
+ * (Equal shares of all rows' chunks, which begin and end inside rows, cost a second set of alternatives in every workgroup:
+ * 4001 rows of 25001 with five 103 us, so 85, and 2055 of 50257 with one 80 and 76.)
  *
  * The n largest: a wave keeps its best 64 in order, one per lane, as 64-bit keys (the logit's bits in an order of whole
  * numbers, then the index from the top, so that equal logits go by index).  Logits that pass the n-th key, which after
@@ -14,11 +15,11 @@
  * over the wave.  The first chunk's threshold is the n-th largest of the lanes' maxima, which n logits reach.  A single
  * alternative is a lane's largest and needs none of this.
  *
- * Bound by HBM and, less so, by the vector ALUs where rows are many: 2055 rows of 50257, 413 MB, 73 us without alternatives
- * (5.6 TB/s; some fifteen instructions a logit), 79 with one, 93 with five, 801 rows of 128256 with 64 105 us.  Few rows are
- * two launches' latency: one row of 128256 with five alternatives 12, 64 rows with none 13, with 20 22.  A bar of the
- * workgroup's own for the alternatives, from what its waves have seen, took 23 of 128 us off 801 rows with 64, and 1.5 of 24
- * off 64 with 20; the passing logits' registers skipped one by one 20 of 123 off 4001 rows of 25001 with five.
+ * Bound by HBM where rows are many: 2055 rows of 50257, 413 MB, 70 to 72 us without alternatives (5.8 TB/s; eleven
+ * instructions a logit), 75 with one, 82 with five, where the networks begin to count: 801 rows of 128256 with 64 95.  Few rows are two
+ * launches' latency: one row of 128256 with five alternatives 10.8, 64 rows with none 12, with 20 20.  A bar of the
+ * workgroup's own for the alternatives, from what its waves have seen, took 23 of 128 us off 801 rows with 64; the registers
+ * without a passing logit skipped one by one 20 of 123 off 4001 rows of 25001 with five.
  *
  * exp((l - m) / T) is taken as exp2((l - m) * (log2 e / T)): one rounding of the product, 2^-24 |l - m| / T relative.
  */
@@ -39,20 +40,9 @@ struct LogStat {
     int32_t ranked, before;
 };
 struct LogPlan {
-    uint32_t all, chunks;                     /* chunks of the line (at most 2^32 - 1), and of a row */
-    int32_t shares;
-    uint32_t each, rest;                      /* all / shares, all % shares */
-    key64* keys;                              /* [2 * shares][n_top] */
-    LogStat* stats;                           /* [2 * shares] */
-    /* Share w's first chunk.  A row that lies in several shares leaves a part in each: the first in slot 2 w + 1, the others
-       in 2 w. */
-    __device__ __forceinline__ uint32_t start(int w) const { return each * w + rest * w / shares; }
-    __device__ __forceinline__ int share_of(uint32_t x) const {
-        int w = min((int)((double)x / (double)all * shares), shares - 1);
-        while (w > 0 && start(w) > x) --w;
-        while (w + 1 < shares && start(w + 1) <= x) ++w;
-        return w;
-    }
+    int32_t parts, chunks;                    /* of a row */
+    key64* keys;                              /* [n_rows][parts][n_top] */
+    LogStat* stats;                           /* [n_rows][parts] */
 };
 
 /* NaN counts as -inf. */
@@ -251,196 +241,170 @@ template <int VU, int TOP>
 __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_logprobs(wsr_logprobs p, LogPlan pl) {
     constexpr int CHUNK = LT * VU * 4;
     __shared__ key64 room[TOP > 1 ? LW : 1][ROOM];
-    __shared__ key64 lists[2][LW][TOP > 0 ? TOP : 1];          /* by the parity of the part, so that one barrier a part is enough */
-    __shared__ LogStat sums[2][LW];
-    __shared__ float quarter[2][LW];                            /* the n / 4-th largest logit that each wave has seen of the part */
+    __shared__ key64 lists[LW][TOP > 0 ? TOP : 1];
+    __shared__ LogStat sums[LW];
+    __shared__ float quarter[LW];                               /* the n / 4-th largest logit that each wave has seen */
     const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), n = (int)p.vocab;
-    uint32_t at = pl.start(blockIdx.x);
-    const uint32_t end = pl.start(blockIdx.x + 1);
-    if (at >= end) return;
-    int64_t r = at / pl.chunks;
-    const int chunks = (int)pl.chunks;
-    int c = (int)(at % pl.chunks);
-    const char* row = (const char*)p.logits + r * p.row_stride;
+    const int64_t r = blockIdx.x / (uint32_t)pl.parts;
+    const int part = (int)(blockIdx.x % (uint32_t)pl.parts);
+    const int begin = part * pl.chunks / pl.parts, end = (part + 1) * pl.chunks / pl.parts;
+    const float* row = (const float*)((const char*)p.logits + r * p.row_stride);
+    const int token = p.tokens ? p.tokens[r] : -1;
+    const float t = temperature_of(p, r);
     float next[VU][4];
-    auto load = [&](const float* from, int chunk) __attribute__((always_inline)) {
+    auto load = [&](int chunk) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < VU; ++u) {
             const int i = chunk * CHUNK + (u * LT + (int)threadIdx.x) * 4;
             if (i + 4 <= n) {
                 /* read once: 2055 rows of 50257 87.8 us without the hint, so 81 */
-                const f4_t q = __builtin_nontemporal_load((const wsr_step::f4_any_t*)(from + i));
+                const f4_t q = __builtin_nontemporal_load((const wsr_step::f4_any_t*)(row + i));
 #pragma unroll
                 for (int j = 0; j < 4; ++j) next[u][j] = q[j];
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) next[u][j] = i + j < n ? from[i + j] : NEG_INF;
+                for (int j = 0; j < 4; ++j) next[u][j] = i + j < n ? row[i + j] : NEG_INF;
             }
         }
     };
-    int token = p.tokens ? p.tokens[r] : -1;
-    float t = temperature_of(p, r);
-    load((const float*)row, c);
-    Best<(TOP > 1 ? TOP : 2)> b;
+    load(begin);
+    const float k = factor_of(t);
+    const bool ranked = token >= 0 && token < n;
+    const float mine = ranked ? no_nan(row[token]) : __builtin_inff();
     const int fourth = (p.n_top + LW - 1) / LW - 1;
-    if constexpr (TOP > 1) {
-        if (lane == 0) quarter[0][wave] = quarter[1][wave] = NEG_INF;
-        __syncthreads();
-    }
-    /* a part: chunks of one row */
+    float m = NEG_INF, s = 0.f, e = 0.f, one = NEG_INF;
+    int before = 0, one_at = 0x7fffffff;
+    Best<(TOP > 1 ? TOP : 2)> b;
+    if constexpr (TOP > 1) b.init(room[wave], p.n_top);
 #pragma unroll 1
-    for (int parity = 0; at < end; parity ^= 1) {
-        const bool head = c == 0;
-        const float k = factor_of(t);
-        const bool ranked = token >= 0 && token < n;
-        const float mine = ranked ? no_nan(((const float*)row)[token]) : __builtin_inff();
-        float m = NEG_INF, s = 0.f, e = 0.f, one = NEG_INF;
-        int before = 0, one_at = 0x7fffffff;
-        if constexpr (TOP > 1) {
-            b.init(room[wave], p.n_top);
-            if (lane == 0) quarter[parity ^ 1][wave] = NEG_INF;  /* for the next part: the last one's waves are all past it */
+    for (int c = begin; c < end; ++c) {
+        float v[VU][4];
+#pragma unroll
+        for (int u = 0; u < VU; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[u][j] = no_nan(next[u][j]);
+        if (c + 1 < end) load(c + 1);
+        const int i0 = c * CHUNK + (int)threadIdx.x * 4;
+        float top = v[0][0];
+#pragma unroll
+        for (int u = 0; u < VU; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, v[u][j]);
+        if (top > m) move_max(m, s, e, top, k);
+        if (__ballot(m == __builtin_inff())) {
+#pragma unroll
+            for (int u = 0; u < VU; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float x = v[u][j] == m ? 0.f : fmaxf((v[u][j] - m) * k, -200.f), f = v[u][j] > NEG_INF ? __builtin_amdgcn_exp2f(x) : 0.f;
+                    s += f;
+                    e = fmaf(f, x, e);
+                }
+        } else {
+            /* -inf gives 2^-200, which is 0, and 0 times -200 */
+            const float base = m == NEG_INF ? 0.f : m;
+#pragma unroll
+            for (int u = 0; u < VU; ++u)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float x = fmaxf((v[u][j] - base) * k, -200.f), f = __builtin_amdgcn_exp2f(x);
+                    s += f;
+                    e = fmaf(f, x, e);
+                }
         }
-#pragma unroll 1
-        for (bool first = true; at < end && c < chunks; first = false, ++at, ++c) {
-            float v[VU][4];
+        /* logits before the given token come before it where they equal its, those behind it do not */
+        if (c * CHUNK + CHUNK <= token) {
 #pragma unroll
             for (int u = 0; u < VU; ++u)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[u][j] = no_nan(next[u][j]);
-            if (at + 1 < end) load((const float*)(c + 1 < chunks ? row : row + p.row_stride), c + 1 < chunks ? c + 1 : 0);
-            const int i0 = c * CHUNK + (int)threadIdx.x * 4;
-            float top = v[0][0];
+                for (int j = 0; j < 4; ++j) before += __builtin_popcountll(__ballot(v[u][j] >= mine));
+        } else if (c * CHUNK > token) {
 #pragma unroll
             for (int u = 0; u < VU; ++u)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) top = fmaxf(top, v[u][j]);
-            if (top > m) move_max(m, s, e, top, k);
-            if (__ballot(m == __builtin_inff())) {
+                for (int j = 0; j < 4; ++j) before += __builtin_popcountll(__ballot(v[u][j] > mine));
+        } else {
 #pragma unroll
-                for (int u = 0; u < VU; ++u)
+            for (int u = 0; u < VU; ++u)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float x = v[u][j] == m ? 0.f : fmaxf((v[u][j] - m) * k, -200.f), f = v[u][j] > NEG_INF ? __builtin_amdgcn_exp2f(x) : 0.f;
-                        s += f;
-                        e = fmaf(f, x, e);
-                    }
-            } else {
-                /* -inf gives 2^-200, which is 0, and 0 times -200 */
-                const float base = m == NEG_INF ? 0.f : m;
-#pragma unroll
-                for (int u = 0; u < VU; ++u)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float x = fmaxf((v[u][j] - base) * k, -200.f), f = __builtin_amdgcn_exp2f(x);
-                        s += f;
-                        e = fmaf(f, x, e);
-                    }
-            }
-            /* logits before the given token come before it where they equal its, those behind it do not */
-            if (c * CHUNK + CHUNK <= token) {
-#pragma unroll
-                for (int u = 0; u < VU; ++u)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) before += __builtin_popcountll(__ballot(v[u][j] >= mine));
-            } else if (c * CHUNK > token) {
-#pragma unroll
-                for (int u = 0; u < VU; ++u)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) before += __builtin_popcountll(__ballot(v[u][j] > mine));
-            } else {
+                for (int j = 0; j < 4; ++j)
+                    before += __builtin_popcountll(__ballot(v[u][j] > mine || (v[u][j] == mine && i0 + u * LT * 4 + j < token)));
+        }
+        if constexpr (TOP == 1) {
+            if (__ballot(top > one))
 #pragma unroll
                 for (int u = 0; u < VU; ++u)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        before += __builtin_popcountll(__ballot(v[u][j] > mine || (v[u][j] == mine && i0 + u * LT * 4 + j < token)));
-            }
-            if constexpr (TOP == 1) {
-                if (__ballot(top > one))
-#pragma unroll
-                    for (int u = 0; u < VU; ++u)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (v[u][j] > one) one = v[u][j], one_at = i0 + u * LT * 4 + j;
-            }
-            if constexpr (TOP > 1) {
-                if (first) {
-                    const int order = __builtin_bit_cast(int, sorted<WAVE>(top, true, lane));
-                    const float bar = __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, p.n_top - 1));
-                    if (bar > NEG_INF) b.raise(key_of(bar, -1));
-                    if (lane == 0) quarter[parity][wave] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, fourth));
-                    __syncthreads();
-                }
-                /* four waves that have seen n / 4 logits of at least this: no smaller one is among the workgroup's n */
-                float common = quarter[parity][0];
-#pragma unroll
-                for (int w = 1; w < LW; ++w) common = fminf(common, quarter[parity][w]);
-                if (common > b.bar) b.raise(key_of(common, -1));
-                if (__ballot(top >= b.bar && top > NEG_INF))
-#pragma unroll
-                    for (int u = 0; u < VU; ++u) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (__ballot(v[u][j] >= b.bar)) b.add(key_of(v[u][j], i0 + u * LT * 4 + j), v[u][j] > NEG_INF, lane);
-                        if (b.drain(lane) && lane == fourth) quarter[parity][wave] = logit_of(b.best);
-                    }
-            }
-        }
-        /* a wave's results, then the workgroup's */
-        move_max(m, s, e, wsr_step::wave_max(m), k);
-        s = wsr::wave_sum(s), e = wsr::wave_sum(e);
-        if constexpr (TOP == 1) {
-            const float top = wsr_step::wave_max(one);
-            const int where = wsr_step::wave_min(one == top ? one_at : 0x7fffffff);
-            if (lane == 0) lists[parity][wave][0] = top > NEG_INF ? key_of(top, where) : 0;
+                        if (v[u][j] > one) one = v[u][j], one_at = i0 + u * LT * 4 + j;
         }
         if constexpr (TOP > 1) {
-            b.flush(lane);
-            if (lane < TOP) lists[parity][wave][lane] = b.best;
-        }
-        if (lane == 0) sums[parity][wave] = LogStat{m, s, e, mine, ranked, before};
-        __syncthreads();
-        if (wave == 0) {
-            LogStat st = sums[parity][0];
-            for (int w = 1; w < LW; ++w) join_stats(st, sums[parity][w], k);
-            key64 best = 0;
-            if constexpr (TOP > 0) best = largest_of<TOP, 1>(LW, lane, [&](int i, int j) { return i < LW ? lists[parity][i][j] : 0; });
-            if (head && c == chunks) {
-                finish(p, r, t, st, best, lane);
-            } else {
-                const int64_t slot = 2 * (int64_t)blockIdx.x + head;
-                if (TOP && lane < p.n_top) pl.keys[slot * p.n_top + lane] = best;
-                if (lane == 0) pl.stats[slot] = st;
+            if (c == begin) {
+                const int order = __builtin_bit_cast(int, sorted<WAVE>(top, true, lane));
+                const float bar = __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, p.n_top - 1));
+                if (bar > NEG_INF) b.raise(key_of(bar, -1));
+                if (lane == 0) quarter[wave] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, fourth));
+                __syncthreads();
             }
+            /* four waves that have seen n / 4 logits of at least this: no smaller one is among the workgroup's n */
+            float common = quarter[0];
+#pragma unroll
+            for (int w = 1; w < LW; ++w) common = fminf(common, quarter[w]);
+            if (common > b.bar) b.raise(key_of(common, -1));
+            if (__ballot(top >= b.bar && top > NEG_INF))
+#pragma unroll
+                for (int u = 0; u < VU; ++u) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (__ballot(v[u][j] >= b.bar)) b.add(key_of(v[u][j], i0 + u * LT * 4 + j), v[u][j] > NEG_INF, lane);
+                    if (b.drain(lane) && lane == fourth) quarter[wave] = logit_of(b.best);
+                }
         }
-        if (c < chunks || at >= end) break;
-        c = 0, ++r, row += p.row_stride;
-        token = p.tokens ? p.tokens[r] : -1;
-        t = temperature_of(p, r);
+    }
+    /* a wave's results, then the workgroup's */
+    move_max(m, s, e, wsr_step::wave_max(m), k);
+    s = wsr::wave_sum(s), e = wsr::wave_sum(e);
+    if constexpr (TOP == 1) {
+        const float top = wsr_step::wave_max(one);
+        const int where = wsr_step::wave_min(one == top ? one_at : 0x7fffffff);
+        if (lane == 0) lists[wave][0] = top > NEG_INF ? key_of(top, where) : 0;
+    }
+    if constexpr (TOP > 1) {
+        b.flush(lane);
+        if (lane < TOP) lists[wave][lane] = b.best;
+    }
+    if (lane == 0) sums[wave] = LogStat{m, s, e, mine, ranked, before};
+    __syncthreads();
+    if (wave) return;
+    LogStat st = sums[0];
+    for (int w = 1; w < LW; ++w) join_stats(st, sums[w], k);
+    key64 best = 0;
+    if constexpr (TOP > 0) best = largest_of<TOP, 1>(LW, lane, [&](int i, int j) { return i < LW ? lists[i][j] : 0; });
+    if (pl.parts == 1) {
+        finish(p, r, t, st, best, lane);
+    } else {
+        if (TOP && lane < p.n_top) pl.keys[(int64_t)blockIdx.x * p.n_top + lane] = best;
+        if (lane == 0) pl.stats[blockIdx.x] = st;
     }
 }
 
-/* Rows that lie in several shares, by the share that the first border inside them ends; a wave takes every fourth part. */
+/* A row's parts; a wave takes every fourth. */
 template <int TOP>
 __global__ __launch_bounds__(LT) void k_logprobs_join(wsr_logprobs p, LogPlan pl) {
     __shared__ key64 lists[LW][TOP > 0 ? TOP : 1];
     __shared__ LogStat sums[LW];
-    const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), w0 = blockIdx.x;
-    const uint32_t border = pl.start(w0 + 1), row0 = border / pl.chunks * pl.chunks;
-    if (border == row0 || pl.start(w0) > row0) return;
-    const int64_t r = row0 / pl.chunks;
-    const int parts = pl.share_of(row0 + pl.chunks - 1) - w0 + 1;
-    auto slot = [&](int i) { return 2 * (int64_t)(w0 + i) + (i == 0); };
+    const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), parts = pl.parts;
+    const int64_t r = blockIdx.x, at = r * parts;
     const float t = temperature_of(p, r), k = factor_of(t);
-    LogStat st = pl.stats[slot(0)];
+    LogStat st = pl.stats[at];
     if (threadIdx.x) st.m = NEG_INF, st.s = 0.f, st.e = 0.f, st.before = 0;
-    for (int i = threadIdx.x ? threadIdx.x : LT; i < parts; i += LT) join_stats(st, pl.stats[slot(i)], k);
+    for (int i = threadIdx.x ? threadIdx.x : LT; i < parts; i += LT) join_stats(st, pl.stats[at + i], k);
     key64 best = 0;
     if constexpr (TOP > 0)
         best = largest_of<TOP, LW>(parts - wave, lane, [&](int i, int j) {
-            return i + wave < parts && j < p.n_top ? pl.keys[slot(i + wave) * p.n_top + j] : 0;
+            return i + wave < parts && j < p.n_top ? pl.keys[(at + i + wave) * p.n_top + j] : 0;
         });
-    const float top = wsr_step::wave_max(st.m);
-    move_max(st.m, st.s, st.e, top, k);
+    move_max(st.m, st.s, st.e, wsr_step::wave_max(st.m), k);
     st.s = wsr::wave_sum(st.s), st.e = wsr::wave_sum(st.e);
 #pragma unroll
     for (int d = 32; d; d >>= 1) st.before += __shfl_xor(st.before, d);
@@ -456,17 +420,19 @@ __global__ __launch_bounds__(LT) void k_logprobs_join(wsr_logprobs p, LogPlan pl
 /* ---- host ------------------------------------------------------------------------------------------ */
 
 constexpr int VU = 4, CHUNK = LT * VU * 4;
-constexpr int LEAST = 4;                      /* chunks of a share at least, once there are 256 of them */
-constexpr int SHARES = 1536;                  /* workgroups that the chip holds: six waves per SIMD */
-
+constexpr int HELD = 1536;                    /* workgroups that the chip holds: six waves per SIMD */
+/* Rows are cut into parts of four chunks or more while those are no more than the chip holds, of eight up to twice as many (801
+   rows of 128256 75 us whole, in three parts 71; 1000 rows of 32000 31 whole, in two parts of four chunks 38), and into
+   shorter ones where they would be fewer than one for each CU. */
 static LogPlan plan_of(const wsr_logprobs& p, void* ws, size_t* bytes) {
     LogPlan pl;
-    pl.chunks = (uint32_t)((p.vocab + CHUNK - 1) / CHUNK);
-    pl.all = (uint32_t)std::min<int64_t>(p.n_rows * pl.chunks, UINT32_MAX);
-    pl.shares = (int32_t)std::max<uint32_t>(1, std::min<uint32_t>(SHARES, std::max<uint32_t>(std::min<uint32_t>(pl.all, 256), pl.all / LEAST)));
-    pl.each = pl.all / pl.shares, pl.rest = pl.all % pl.shares;
-    const size_t slots = 2 * (size_t)pl.shares, keys = (slots * p.n_top * sizeof(key64) + 255) / 256 * 256;
-    if (bytes) *bytes = keys + slots * sizeof(LogStat);
+    const int64_t chunks = (p.vocab + CHUNK - 1) / CHUNK, rows = std::max<int64_t>(1, p.n_rows);
+    const int64_t parts = std::max({std::min(chunks / 4, HELD / rows), std::min(chunks / 8, 2 * HELD / rows),
+                                    std::min(chunks, (256 + rows - 1) / rows)});
+    pl.chunks = (int32_t)chunks;
+    pl.parts = (int32_t)std::max<int64_t>(1, parts);
+    const size_t items = (size_t)p.n_rows * pl.parts, keys = (items * p.n_top * sizeof(key64) + 255) / 256 * 256;
+    if (bytes) *bytes = pl.parts == 1 ? 256 : keys + items * sizeof(LogStat);
     pl.keys = static_cast<key64*>(ws);
     pl.stats = reinterpret_cast<LogStat*>(static_cast<char*>(ws) + keys);
     return pl;
@@ -480,10 +446,10 @@ size_t logprobs_workspace(const wsr_logprobs& p) {
 
 template <int TOP>
 static hipError_t launch_top(const wsr_logprobs& p, const LogPlan& pl, hipStream_t s) {
-    hipLaunchKernelGGL((k_logprobs<VU, TOP>), dim3((unsigned)pl.shares), dim3(LT), 0, s, p, pl);
+    hipLaunchKernelGGL((k_logprobs<VU, TOP>), dim3((unsigned)(p.n_rows * pl.parts)), dim3(LT), 0, s, p, pl);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || pl.chunks == 1 || (pl.rest == 0 && pl.each % pl.chunks == 0)) return e;
-    hipLaunchKernelGGL(k_logprobs_join<TOP>, dim3((unsigned)pl.shares - 1), dim3(LT), 0, s, p, pl);
+    if (e != hipSuccess || pl.parts == 1) return e;
+    hipLaunchKernelGGL(k_logprobs_join<TOP>, dim3((unsigned)p.n_rows), dim3(LT), 0, s, p, pl);
     return hipGetLastError();
 }
 

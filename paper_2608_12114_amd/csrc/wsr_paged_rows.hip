@@ -110,7 +110,8 @@ __global__ __launch_bounds__(AT) __attribute__((amdgpu_waves_per_eu(2))) void k_
     Place place;
     if (!find(p, pl, blockIdx.x, false, place)) return;
     const Seq s = place.s;
-    const int parts = place.parts, part = place.at % parts, unit = place.at / parts, head = unit % N, tile = unit / N;
+    /* key heads side by side: of eight of them each stays on one XCD, whose L2 holds the keys that its tiles share */
+    const int parts = place.parts, head = place.at % N, part = place.at / N % parts, tile = place.at / N / parts;
     const int row0 = tile * R, last = min(row0 + R, s.rows) - 1, past = s.len - s.n;
     const int seen = max(past + last / G + 1, 0);
     const int each = ((seen + parts - 1) / parts + STEP - 1) / STEP * STEP;
@@ -186,7 +187,7 @@ __global__ __launch_bounds__(AT) __attribute__((amdgpu_waves_per_eu(2))) void k_
                     u32x2{pack2<FMT>(a.o[i][4 * j] * inv, a.o[i][4 * j + 1] * inv), pack2<FMT>(a.o[i][4 * j + 2] * inv, a.o[i][4 * j + 3] * inv)};
         if (p.lse && h == 0) p.lse[(int64_t)tok * p.n_heads + qh] = lse_of(a.m, a.l, p.scale);
     } else {
-        const int to_slot = place.slot + place.at;
+        const int to_slot = place.slot + (tile * N + head) * parts + part;
         if (to_slot >= pl.slots) return;
         float* w = pl.part + ((int64_t)to_slot * R + row - row0) * (D + 4);
 #pragma unroll
