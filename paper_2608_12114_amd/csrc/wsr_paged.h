@@ -38,10 +38,12 @@ __device__ __forceinline__ Seq seq_at(const wsr_paged& p, int R, int b) {
     return s;
 }
 
-/* Keys of a part, at most: as many as leave one part for each workgroup that the chip holds beside those that the units'
-   ends cost, of LEAST or more.  Sums of lengths in fp32, which every wave rounds alike. */
-constexpr float LEAST = 256.f;
-constexpr float ROUNDS = 2.f;
+/* Where units are few against the workgroups that the chip holds, an eighth of them, or half for tiles of more than 32 rows,
+   they are cut into as many parts as fill it once, the shorter ones rounded up (7 sequences of up to 65536 keys 257 us, in one and
+   a half rounds 267; 24 of 5 drafts of 8 heads 69, by the other rule 75).  Otherwise parts are half of what falls to a
+   workgroup, and units of less than two such stay whole, so that whoever is done early takes another (16 sequences of 2000
+   with 32 key heads 59 us, by the first rule 69).  A part has 256 keys or more, of 64 (128) rows 448 (704), since its rows have
+   to be written and read again.  Sums of lengths are fp32, which every wave rounds alike. */
 struct Sums {
     float keys, units;
     __device__ __forceinline__ void add(const Seq& s, int N) { units += (float)s.tiles * N, keys += (float)s.tiles * N * s.len; }
@@ -50,13 +52,13 @@ struct Cut {
     float part, up;                           /* keys of a part; what is added before the number of parts is rounded down */
 };
 __device__ __forceinline__ Cut cut_of(const PagedPlan& pl, const Sums& s) {
-    const float held = (float)pl.held, least = LEAST + 4.f * (pl.rows - 16);
+    const float held = (float)pl.held, least = 192.f + 4.f * pl.rows;
     return s.units <= held * (pl.rows > 32 ? 0.5f : 0.125f) ? Cut{fmaxf(least, s.keys / (held - s.units)), 0.999f}
-                                                            : Cut{fmaxf(least, s.keys / (held * ROUNDS)), 0.f};
+                                                            : Cut{fmaxf(least, s.keys / (held * 2.f)), 0.f};
 }
 /* Parts of each of a sequence's units. */
 __device__ __forceinline__ int parts_of(const Seq& s, Cut cut) {
-    return (int)fminf(fmaxf(floorf((float)s.len / cut.part + cut.up), 1.f), 65536.f);
+    return (int)fminf(fmaxf(floorf((float)s.len / cut.part + cut.up), 1.f), 2048.f);
 }
 
 /* The lanes' sums of themselves and those below: inside 16-lane rows, then the rows' last lanes handed on. */

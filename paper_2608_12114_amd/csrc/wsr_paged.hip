@@ -15,7 +15,13 @@
  *
  * Keys and values are loaded as whole rows, a wave's 64 lanes of 16 bytes side by side, into registers, which hold more on
  * their way than LDS could, and turned into operands by the wave's own 32 rows of LDS: first the keys, then, by transposing
- * reads, the values.  No wave waits for another before the end, where those of a workgroup, who take blocks in turn, add up.
+ * reads, the values.  (Loaded straight in operand layout, 64 bytes of 16 keys at a time, 7 sequences of up to 65536 keys took
+ * 295 us, so 259; and whole rows gain from the hint that they are read once, 292 without it, which the others lose by.)  No wave
+ * waits for another before the end, where those of a workgroup, who take blocks in turn, add up.
+ *
+ * Bound by HBM: those 7, 1577 MB of keys, 248 us (6.4 TB/s), 32 of up to 4096 62 (320 MB, 5.1 TB/s).  Short ones are
+ * latency, lengths, pages, keys and the join in turn: one of 500 keys 8.1 us, one of 2000 12, 32771 31 (134 MB).
+ * Tiles of 64 and 128 rows: wsr_paged_rows.hip.
  */
 #include <hip/hip_runtime.h>
 
@@ -449,13 +455,20 @@ __global__ __launch_bounds__(JT) void k_paged_join(wsr_paged p, PagedPlan pl) {
 
 /* ---- host ------------------------------------------------------------------------------------------ */
 
-constexpr int WIDE = 256;
-constexpr int FEW = 2048;
+/* Sequences times key heads below which units are few: one launch then pays up to 768 keys (one sequence of 500 11.7 us in
+   two, 8.1 in one with twelve waves a unit; of 1000 11.5 and 11.8), and beyond it up to 1536 (63 of 1000 33.4 us in two, 31 in
+   one; 64 of 500 25.8 and 18.5, with twelve waves a unit 19.7). */
+constexpr int FEW_UNITS = 256;
+/* Rows up to which a row's parts are joined by four waves: 32 rows of 86 parts 15 us by one wave each, so 6. */
+constexpr int FEW_ROWS = 2048;
 
-/* Rows of a tile: as many as a sequence's fill, on average. */
+/* Rows of a tile: as many as a sequence's fill, on average; 128 where there are tiles enough of them (a chunk of 512 tokens of
+   32 heads on 8, 128 tiles, 18.6 us with 128 rows and 15.5 with 64; two of up to 512 behind 4096, 216 tiles, 78 and 87). */
 static int tile_rows(const wsr_paged& p) {
     const int64_t rows = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads), n = p.n_seqs;
-    return rows <= 16 * n ? 16 : rows <= 32 * n || p.head_dim == 256 ? 32 : rows <= 64 * n ? 64 : 128;
+    if (rows <= 16 * n) return 16;
+    if (rows <= 32 * n || p.head_dim == 256) return 32;
+    return rows <= 64 * n || p.n_kv_heads * (rows / 128) < 160 ? 64 : 128;
 }
 
 static PagedPlan paged_plan(const wsr_paged& p) {
@@ -463,7 +476,7 @@ static PagedPlan paged_plan(const wsr_paged& p) {
     pl.rows = tile_rows(p);
     pl.held = 256 * (pl.rows > 32 ? 2 : waves_of(p.head_dim, pl.rows / 16));
     pl.slots = 4 * pl.held;
-    pl.whole = p.max_len <= ((int64_t)p.n_kv_heads * std::min(p.n_seqs, p.n_tokens) < WIDE ? 768 : 1536);
+    pl.whole = p.max_len <= ((int64_t)p.n_kv_heads * std::min(p.n_seqs, p.n_tokens) < FEW_UNITS ? 768 : 1536);
     /* n / d = (n * M) >> (31 + s), 2^s >= d, M = 2^(31 + s) / d + 1, for n < 2^31: M d is over 2^(31 + s) by at most d */
     int s = 0;
     while ((int64_t)1 << s < p.cache.page_size) ++s;
@@ -496,7 +509,7 @@ static hipError_t launch_dim(const wsr_paged& p, const PagedPlan& pl, hipStream_
     if (pl.rows > 32) {
         e = launch_paged_rows(p, pl, pl.rows / 32, once, blocks, s);
     } else {
-        if (pl.rows == 16 && pl.whole && D < 256 && (int64_t)p.n_kv_heads * p.n_seqs < WIDE)
+        if (pl.rows == 16 && pl.whole && D < 256 && (int64_t)p.n_kv_heads * p.n_seqs < FEW_UNITS)
             hipLaunchKernelGGL((k_paged<FMT, D, 1, (D < 256 ? 12 : 4), true>), grid, dim3(12 * WAVE), 0, s, p, pl);
         else if (pl.rows == 16) hipLaunchKernelGGL((k_paged<FMT, D, 1, 4, true>), grid, threads, 0, s, p, pl);
         else if (once) hipLaunchKernelGGL((k_paged<FMT, D, 2, 4, true>), grid, threads, 0, s, p, pl);
@@ -505,7 +518,7 @@ static hipError_t launch_dim(const wsr_paged& p, const PagedPlan& pl, hipStream_
     }
     if (e != hipSuccess || pl.whole) return e;
     const int64_t rows = (int64_t)p.n_tokens * p.n_heads;       /* at most 2^25: one launch */
-    if (rows <= FEW) hipLaunchKernelGGL((k_paged_join<FMT, D, JW>), dim3((unsigned)rows), dim3(JT), 0, s, p, pl);
+    if (rows <= FEW_ROWS) hipLaunchKernelGGL((k_paged_join<FMT, D, JW>), dim3((unsigned)rows), dim3(JT), 0, s, p, pl);
     else hipLaunchKernelGGL((k_paged_join<FMT, D, 1>), dim3((unsigned)((rows + JW - 1) / JW)), dim3(JT), 0, s, p, pl);
     return hipGetLastError();
 }
