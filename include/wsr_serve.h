@@ -98,11 +98,12 @@ wsr_status wsr_append_qkv(const wsr_qkv* p, void* stream);
    statistics and sums are fp32, probabilities are rounded to `fmt` for the product with the values, out once to `fmt`.
    Rows of q that belong to no sequence (before starts[0], from starts[n_seqs] on) keep what out and lse held.
    starts: device int32 [n_seqs + 1], not decreasing, clamped to [0, n_tokens]; lens: device int32 [n_seqs], clamped to
-   [0, max_len];
-   max_len <= max_pages * page_size.  n_tokens and n_seqs at most 2^20, n_heads at most 4096, tokens times
-   heads at most 2^25; n_kv_heads * (n_seqs + a key head's rows / 16) past 2^23 may be refused.  head_dim 64, 128 or 256; every pointer 16-byte aligned and every stride a
-   multiple of 16 (of 4 for table, starts, lens and lse); lse (n_tokens, n_heads) or null.  ws:
-   wsr_paged_workspace_bytes(), 256-byte aligned. */
+   [0, max_len]; max_len <= max_pages * page_size.  n_tokens and n_seqs at most 2^20, n_heads at most 4096, tokens
+   times heads at most 2^25; n_kv_heads * (n_seqs + a key head's rows / 16) past 2^23 may be refused.  head_dim 64, 128
+   or 256; every pointer 16-byte aligned and every stride a multiple of 16 (of 4 for table, starts, lens and lse); lse
+   (n_tokens, n_heads) or null; out and lse overlap nothing.  ws: wsr_paged_workspace_bytes() of the call's own sizes
+   (more tokens to a sequence may take more, or less), 256-byte aligned.  Sums of probabilities, relative to within 2^8 of
+   the largest, times values are infinite past fp32's range. */
 typedef struct wsr_paged {
     int32_t fmt, n_heads, n_kv_heads, head_dim, n_seqs, n_tokens;
     float scale;
@@ -123,7 +124,7 @@ wsr_status wsr_paged_attention(const wsr_paged* p, void* ws, size_t ws_bytes, vo
 
    Of each row of logits, with p = softmax(logits / T), T = temperature[r] (null: 1; T = 0, infinite logits and NaN as in
    wsr_verify: a NaN counts as -inf, +inf as sharing all of the probability, T = 0 and what is not above 0 puts all of it on
-   the lowest index of the largest logit, T above 1e30 is 1e30):
+   the lowest index of the largest logit, T above 1e30 is 1e30, below 2^-126 is 2^-126):
      logp[r]      log p of tokens[r]                      rank[r]     how many tokens come before it
      entropy[r]   - sum p log p
      top[r]       the n_top tokens that come first, in order, and top_logp[r] their log p

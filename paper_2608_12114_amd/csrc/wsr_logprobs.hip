@@ -59,7 +59,7 @@ __device__ __forceinline__ int index_of(key64 k) { return (int)(0xffffffffu - (u
 
 __device__ __forceinline__ float temperature_of(const wsr_logprobs& p, int64_t r) {
     const float t = p.temperature ? p.temperature[r] : 1.f;
-    return t > 0.f ? fminf(t, 1e30f) : 0.f;
+    return t > 0.f ? fminf(fmaxf(t, 0x1p-126f), 1e30f) : 0.f;   /* log2 e / T is finite */
 }
 __device__ __forceinline__ float factor_of(float t) { return t > 0.f ? LOG2E / t : 0.f; }
 

@@ -43,18 +43,23 @@ __device__ __forceinline__ Seq seq_at(const wsr_paged& p, int R, int b) {
    a half rounds 267; 24 of 5 drafts of 8 heads 69, by the other rule 75).  Otherwise parts are half of what falls to a
    workgroup, and units of less than two such stay whole, so that whoever is done early takes another (16 sequences of 2000
    with 32 key heads 59 us, by the first rule 69).  A part has 256 keys or more, of 64 (128) rows 448 (704), since its rows have
-   to be written and read again.  Sums of lengths are fp32, which every wave rounds alike. */
+   to be written and read again.  Sums of lengths are fp32, with every product's rounding written out: all waves of both
+   kernels have to cut alike. */
 struct Sums {
     float keys, units;
-    __device__ __forceinline__ void add(const Seq& s, int N) { units += (float)s.tiles * N, keys += (float)s.tiles * N * s.len; }
+    __device__ __forceinline__ void add(const Seq& s, int N) {
+        const float of = (float)(s.tiles * N);
+        units += of, keys = fmaf(of, (float)s.len, keys);
+    }
 };
 struct Cut {
     float part, up;                           /* keys of a part; what is added before the number of parts is rounded down */
 };
+__host__ __device__ __forceinline__ float few_units(const PagedPlan& pl) { return (float)pl.held * (pl.rows > 32 ? 0.5f : 0.125f); }
 __device__ __forceinline__ Cut cut_of(const PagedPlan& pl, const Sums& s) {
-    const float held = (float)pl.held, least = 192.f + 4.f * pl.rows;
-    return s.units <= held * (pl.rows > 32 ? 0.5f : 0.125f) ? Cut{fmaxf(least, s.keys / (held - s.units)), 0.999f}
-                                                            : Cut{fmaxf(least, s.keys / (held * 2.f)), 0.f};
+    const float held = (float)pl.held, least = (float)(192 + 4 * pl.rows);
+    return s.units <= few_units(pl) ? Cut{fmaxf(least, s.keys / (held - s.units)), 0.999f}
+                                    : Cut{fmaxf(least, s.keys / (held * 2.f)), 0.f};
 }
 /* Parts of each of a sequence's units. */
 __device__ __forceinline__ int parts_of(const Seq& s, Cut cut) {

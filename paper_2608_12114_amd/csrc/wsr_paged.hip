@@ -471,11 +471,18 @@ static int tile_rows(const wsr_paged& p) {
     return rows <= 64 * n || p.n_kv_heads * (rows / 128) < 160 ? 64 : 128;
 }
 
+/* Units of a call, at most. */
+static int64_t most_units(const wsr_paged& p, const PagedPlan& pl) {
+    const int64_t rows = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads);
+    return p.n_kv_heads * (rows / pl.rows + std::min(p.n_seqs, p.n_tokens));
+}
+
 static PagedPlan paged_plan(const wsr_paged& p) {
     PagedPlan pl{};
     pl.rows = tile_rows(p);
     pl.held = 256 * (pl.rows > 32 ? 2 : waves_of(p.head_dim, pl.rows / 16));
-    pl.slots = 4 * pl.held;
+    /* parts come to what the chip holds where units are few, to twice that elsewhere, and what fp32 sums may be off by */
+    pl.slots = (most_units(p, pl) <= few_units(pl) ? 1 : 2) * pl.held + 64;
     pl.whole = p.max_len <= ((int64_t)p.n_kv_heads * std::min(p.n_seqs, p.n_tokens) < FEW_UNITS ? 768 : 1536);
     /* n / d = (n * M) >> (31 + s), 2^s >= d, M = 2^(31 + s) / d + 1, for n < 2^31: M d is over 2^(31 + s) by at most d */
     int s = 0;
@@ -488,12 +495,6 @@ static PagedPlan paged_plan(const wsr_paged& p) {
 size_t paged_workspace(const wsr_paged& p) {
     const PagedPlan pl = paged_plan(p);
     return pl.whole ? 256 : (size_t)pl.slots * pl.rows * (p.head_dim + 4) * sizeof(float);
-}
-
-/* Units of a call, at most. */
-static int64_t most_units(const wsr_paged& p, const PagedPlan& pl) {
-    const int64_t rows = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads);
-    return p.n_kv_heads * (rows / pl.rows + std::min(p.n_seqs, p.n_tokens));
 }
 
 /* Workgroups of the first launch. */

@@ -15,7 +15,8 @@ def turned64(x, positions, freqs, axis_of, *, rot, pairs, kind=None, w=None, b=N
     """Heads x (T, h, D) normed and turned, positions (axes, T), and the bound on what fp32 arithmetic adds to the
     rounding.  A norm's sums are trees of fewer than 16 roundings, its factor and weight a few more, so 32 half steps
     of the normed values (of their spread before the mean is taken off); cosine and sine are off by less than 4 half
-    steps of 1 (the fraction's rounding 2^-26 turns, the function's own 2^-23), products and sum by 3 more."""
+    steps of 1 (a rest of at most half a quarter turn rounded to fp32, times a rounded constant, 2^-23.7 in all; the
+    series' own rest and last roundings, 2^-23.8), products and sum by 3 more."""
     x = x.double()
     mag = x.abs()
     if kind is not None:
@@ -108,7 +109,7 @@ def logprobs64(row, token, temperature, n_top):
     V = row.numel()
     v = row.double().cpu()
     v = torch.where(torch.isnan(v), -math.inf, v) + 0.0
-    T = min(temperature, 1e30) if temperature > 0 else 0.0
+    T = min(max(temperature, 2.0 ** -126), 1e30) if temperature > 0 else 0.0
     order = sorted(range(V), key=lambda i: (-v[i].item(), i)) if V <= 4096 else torch.sort(v, descending=True, stable=True).indices.tolist()
     top = v[order[0]].item()
     if top == -math.inf:

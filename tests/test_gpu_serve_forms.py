@@ -89,3 +89,11 @@ def test_one_sequence_beside_many_key_heads():
     c = Case([1, 1], [1400, 1000], 256, 256, 64, BF16)
     c.run()
     c.check()
+
+
+@pytest.mark.parametrize("N,seqs,n,room", [(8, 32, 1, 0), (8, 32, 1, 2500), (7, 19, 1, 0), (8, 16, 1, 0), (8, 8, 17, 0), (4, 8, 24, 0)])
+def test_as_many_parts_as_there_is_room_for(N, seqs, n, room):
+    """Equal lengths, whose units come out in whole parts: all that the workspace holds, on both sides of few units."""
+    c = Case([n] * seqs, [2048] * seqs, 8 * N, N, 64, F16, page=32, room=room)
+    c.run()
+    c.check()

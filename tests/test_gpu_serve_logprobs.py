@@ -109,6 +109,16 @@ def test_temperatures():
     c.check()
 
 
+def test_temperatures_near_zero():
+    """Those whose inverse fp32 does not hold count as the smallest normal one: the largest logits share the probability."""
+    x = _normal(5, 3000, 7)
+    x[:, 11] = x[:, 2999] = x.max() + 1
+    c = Case(x, [11, 2999, 0, 2999, 11], 3, [2.0 ** -149, 1e-40, 1e-39, 2.0 ** -126, 1.5e-38])
+    c.run()
+    c.check()
+    assert (c.logp[[0, 1, 3, 4]] + 0.6931471805599453).abs().max() < 1e-6 and (c.entropy - 0.6931471805599453).abs().max() < 1e-6
+
+
 def test_rows_anywhere():
     """Rows that start at any 4 bytes and are apart; NaN between them is not read."""
     wide = torch.full((9, 5009), NAN, device="cuda")
