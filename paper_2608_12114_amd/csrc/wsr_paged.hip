@@ -374,35 +374,45 @@ __global__ __launch_bounds__(NW * WAVE) __attribute__((amdgpu_waves_per_eu(waves
     }
 }
 
-/* Rows whose unit is cut: W waves per (token, head) take its parts, each several side by side in D / 4 lanes and AHEAD loaded at
-   a time. */
+/* Rows whose unit is cut.  A part's row takes D / 4 lanes: where rows are many, W = 1, a wave has a row in each of its groups of
+   so many lanes (2 chunks of up to 512 tokens 11 us, with one row a wave 16); where they are few, four waves take the parts
+   of one row, a group each.  AHEAD parts are loaded at a time. */
 constexpr int JT = 256, JW = JT / WAVE;
 template <int FMT, int D, int W>
-__global__ __launch_bounds__(JT) void k_paged_join(wsr_paged p, PagedPlan pl) {
-    constexpr int LANES = D / 4, SIDE = WAVE / LANES, AHEAD = 4;
+__global__ __launch_bounds__(JT) __attribute__((amdgpu_waves_per_eu(W == 1 ? 8 : 4))) void k_paged_join(wsr_paged p, PagedPlan pl) {
+    constexpr int LANES = D / 4, SIDE = WAVE / LANES, AHEAD = 4, ROWS = W == 1 ? SIDE : 1, APART = W == 1 ? 1 : SIDE * W;
     __shared__ f4_t sums[JW][LANES];
     __shared__ float stats[JW][2];
-    const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), turn = wave % W, x = lane % LANES;
-    const int64_t at = (int64_t)blockIdx.x * (JW / W) + wave / W;
-    if (at >= (int64_t)p.n_tokens * p.n_heads) return;          /* of W = 4, all of the workgroup */
+    const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), turn = wave % W, group = lane / LANES, x = lane % LANES;
+    const int64_t first = ((int64_t)blockIdx.x * (JW / W) + wave / W) * ROWS, rows = (int64_t)p.n_tokens * p.n_heads;
+    if (first >= rows) return;                                  /* of W = 4, all of the workgroup */
+    const int64_t at = min(first + (W == 1 ? group : 0), rows - 1);
     const int tok = (int)(at / p.n_heads), qh = (int)(at % p.n_heads), G = p.n_heads / p.n_kv_heads, R = pl.rows;
-    const int b = seq_of(p.starts, p.n_seqs, tok).seq;
-    Place o_place;
-    if (b < 0 || !find(p, pl, b, true, o_place) || o_place.parts == 1) return;
-    const int parts = o_place.parts, row = (tok - o_place.s.t0) * G + qh % G;
-    const int slot0 = o_place.slot + (row / R * p.n_kv_heads + qh / G) * parts;
-    if (slot0 < 0 || slot0 + parts > pl.slots) return;
-    const float* from = pl.part + ((int64_t)slot0 * R + row % R) * (D + 4);
+    int parts = 1;
+    const float* from = pl.part;
     const int64_t step = (int64_t)R * (D + 4);
+    const int last = (int)(min(first + ROWS - 1, rows - 1) / p.n_heads);
+    for (int t = (int)(first / p.n_heads); t <= last; ++t) {    /* the wave's tokens, most often one */
+        const int b = seq_of(p.starts, p.n_seqs, t).seq;
+        Place o_place;
+        if (b < 0 || !find(p, pl, b, true, o_place) || o_place.parts == 1 || t != tok) continue;
+        const int row = (tok - o_place.s.t0) * G + qh % G, slot = o_place.slot + (row / R * p.n_kv_heads + qh / G) * o_place.parts;
+        if (slot < 0 || slot + o_place.parts > pl.slots) continue;
+        parts = o_place.parts;
+        from = pl.part + ((int64_t)slot * R + row % R) * (D + 4);
+    }
+    if (__ballot(parts > 1) == 0) return;
+    if (parts == 1) parts = 0;
     const float c = p.scale * LOG2E;
     float m = NEG_INF, l = 0.f;
     f4_t o = f4_t{0.f, 0.f, 0.f, 0.f};
-    for (int i = turn * SIDE + lane / LANES; i - lane / LANES < parts; i += AHEAD * SIDE * W) {
+#pragma unroll 1
+    for (int i = W == 1 ? 0 : turn * SIDE + group; i < parts; i += AHEAD * APART) {
         float pm[AHEAD], ps[AHEAD];
         f4_t po[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
-            const int j = i + k * SIDE * W;
+            const int j = i + k * APART;
             const float* w = from + min(j, parts - 1) * step;
             pm[k] = j < parts ? w[D] : NEG_INF, ps[k] = j < parts ? w[D + 1] : 0.f;
             po[k] = j < parts ? *(const f4_t*)(w + 4 * x) : f4_t{0.f, 0.f, 0.f, 0.f};
@@ -423,34 +433,34 @@ __global__ __launch_bounds__(JT) void k_paged_join(wsr_paged p, PagedPlan pl) {
         }
         m = top;
     }
-    auto add = [&](float m2, float l2, f4_t o2) {
-        const float top = fmaxf(m, m2), base = top == NEG_INF ? 0.f : top * c;
-        const float a = __builtin_amdgcn_exp2f(m * c - base), f = __builtin_amdgcn_exp2f(m2 * c - base);
-        l = l * a + l2 * f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = o[e] * a + o2[e] * f;
-        m = top;
-    };
-#pragma unroll
-    for (int d = LANES; d < WAVE; d *= 2) {
-        f4_t o2;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o2[e] = __shfl_xor(o[e], d);
-        add(__shfl_xor(m, d), __shfl_xor(l, d), o2);
-    }
     if constexpr (W > 1) {
+        auto add = [&](float m2, float l2, f4_t o2) {
+            const float top = fmaxf(m, m2), base = top == NEG_INF ? 0.f : top * c;
+            const float a = __builtin_amdgcn_exp2f(m * c - base), f = __builtin_amdgcn_exp2f(m2 * c - base);
+            l = l * a + l2 * f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = o[e] * a + o2[e] * f;
+            m = top;
+        };
+#pragma unroll
+        for (int d = LANES; d < WAVE; d *= 2) {
+            f4_t o2;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o2[e] = __shfl_xor(o[e], d);
+            add(__shfl_xor(m, d), __shfl_xor(l, d), o2);
+        }
         if (lane < LANES) sums[wave][x] = o;
         if (lane == 0) stats[wave][0] = m, stats[wave][1] = l;
         __syncthreads();
-        if (turn) return;
+        if (turn || lane >= LANES) return;
 #pragma unroll
         for (int w = 1; w < W; ++w) add(stats[w][0], stats[w][1], sums[w][x]);
     }
-    if (lane >= LANES) return;
+    if (parts == 0 || first + (W == 1 ? group : 0) >= rows) return;
     const float inv = inverse_of(l);
     char* out = (char*)p.out + tok * p.out_tok_stride + qh * p.out_head_stride;
     ((u32x2*)out)[x] = u32x2{pack2<FMT>(o[0] * inv, o[1] * inv), pack2<FMT>(o[2] * inv, o[3] * inv)};
-    if (p.lse && lane == 0) p.lse[(int64_t)tok * p.n_heads + qh] = lse_of(m, l, p.scale);
+    if (p.lse && x == 0) p.lse[at] = lse_of(m, l, p.scale);
 }
 
 /* ---- host ------------------------------------------------------------------------------------------ */
@@ -520,7 +530,7 @@ static hipError_t launch_dim(const wsr_paged& p, const PagedPlan& pl, hipStream_
     if (e != hipSuccess || pl.whole) return e;
     const int64_t rows = (int64_t)p.n_tokens * p.n_heads;       /* at most 2^25: one launch */
     if (rows <= FEW_ROWS) hipLaunchKernelGGL((k_paged_join<FMT, D, JW>), dim3((unsigned)rows), dim3(JT), 0, s, p, pl);
-    else hipLaunchKernelGGL((k_paged_join<FMT, D, 1>), dim3((unsigned)((rows + JW - 1) / JW)), dim3(JT), 0, s, p, pl);
+    else hipLaunchKernelGGL((k_paged_join<FMT, D, 1>), dim3((unsigned)((rows + JT * 4 / D - 1) / (JT * 4 / D))), dim3(JT), 0, s, p, pl);
     return hipGetLastError();
 }
 
