@@ -101,8 +101,8 @@ wsr_status wsr_append_qkv(const wsr_qkv* p, void* stream);
    [0, max_len]; max_len <= max_pages * page_size.  n_tokens and n_seqs at most 2^20, n_heads at most 4096, tokens
    times heads at most 2^25; n_kv_heads * (n_seqs + a key head's rows / 16) past 2^23 may be refused.  head_dim 64, 128
    or 256; every pointer 16-byte aligned and every stride a multiple of 16 (of 4 for table, starts, lens and lse); lse
-   (n_tokens, n_heads) or null; out and lse overlap nothing.  ws: wsr_paged_workspace_bytes() of the call's own sizes
-   (more tokens to a sequence may take more, or less), 256-byte aligned.  Sums of probabilities, relative to within 2^8 of
+   (n_tokens, n_heads) or null; out and lse overlap nothing.  ws: wsr_paged_workspace_bytes(), 256-byte aligned; what
+   it gives serves calls of fewer tokens too where the rest is the same (without starts, of fewer sequences).  Sums of probabilities, relative to within 2^8 of
    the largest, times values are infinite past fp32's range. */
 typedef struct wsr_paged {
     int32_t fmt, n_heads, n_kv_heads, head_dim, n_seqs, n_tokens;
@@ -136,7 +136,7 @@ wsr_status wsr_paged_attention(const wsr_paged* p, void* ws, size_t ws_bytes, vo
    logits: fp32, 4-byte aligned, row_stride a multiple of 4; tokens: device int32 [n_rows] or null (no logp, no rank);
    logp, rank, entropy and top_logp may be null.  1 <= vocab <= 2^24, 0 <= n_top <= 64, n_rows <= 2^20,
    n_rows * vocab <= 2^40.
-   ws: wsr_logprobs_workspace_bytes(), 256-byte aligned. */
+   ws: wsr_logprobs_workspace_bytes(), 256-byte aligned; what it gives serves calls of fewer rows too. */
 typedef struct wsr_logprobs {
     int64_t n_rows, vocab;
     int32_t n_top;

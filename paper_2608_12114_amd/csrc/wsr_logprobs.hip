@@ -421,27 +421,29 @@ __global__ __launch_bounds__(LT) void k_logprobs_join(wsr_logprobs p, LogPlan pl
 
 constexpr int VU = 4, CHUNK = LT * VU * 4;
 constexpr int HELD = 1536;                    /* workgroups that the chip holds: six waves per SIMD */
+static size_t key_bytes(int64_t items, int32_t n_top) { return (items * n_top * sizeof(key64) + 255) / 256 * 256; }
 /* Rows are cut into parts of four chunks or more while those are no more than the chip holds, of eight up to twice as many (801
    rows of 128256 75 us whole, in three parts 71; 1000 rows of 32000 31 whole, in two parts of four chunks 38), and into
    shorter ones where they would be fewer than one for each CU. */
-static LogPlan plan_of(const wsr_logprobs& p, void* ws, size_t* bytes) {
+static LogPlan plan_of(const wsr_logprobs& p, void* ws) {
     LogPlan pl;
     const int64_t chunks = (p.vocab + CHUNK - 1) / CHUNK, rows = std::max<int64_t>(1, p.n_rows);
     const int64_t parts = std::max({std::min(chunks / 4, HELD / rows), std::min(chunks / 8, 2 * HELD / rows),
                                     std::min(chunks, (256 + rows - 1) / rows)});
     pl.chunks = (int32_t)chunks;
     pl.parts = (int32_t)std::max<int64_t>(1, parts);
-    const size_t items = (size_t)p.n_rows * pl.parts, keys = (items * p.n_top * sizeof(key64) + 255) / 256 * 256;
-    if (bytes) *bytes = pl.parts == 1 ? 256 : keys + items * sizeof(LogStat);
     pl.keys = static_cast<key64*>(ws);
-    pl.stats = reinterpret_cast<LogStat*>(static_cast<char*>(ws) + keys);
+    pl.stats = reinterpret_cast<LogStat*>(static_cast<char*>(ws) + key_bytes(p.n_rows * pl.parts, p.n_top));
     return pl;
 }
 
+/* What the call needs, and any of fewer rows, which may have more parts: as many as plan_of() allows at most. */
 size_t logprobs_workspace(const wsr_logprobs& p) {
-    size_t n;
-    plan_of(p, nullptr, &n);
-    return n;
+    const int64_t chunks = (p.vocab + CHUNK - 1) / CHUNK;
+    if (chunks == 1) return 256;
+    const int64_t items = std::max({std::min(p.n_rows * (chunks / 4), (int64_t)HELD), std::min(p.n_rows * (chunks / 8), (int64_t)2 * HELD),
+                                    std::min(p.n_rows * chunks, (int64_t)511)});
+    return std::max<size_t>(256, key_bytes(items, p.n_top) + items * sizeof(LogStat));
 }
 
 template <int TOP>
@@ -454,7 +456,7 @@ static hipError_t launch_top(const wsr_logprobs& p, const LogPlan& pl, hipStream
 }
 
 hipError_t launch_logprobs(const wsr_logprobs& p, void* ws, hipStream_t s) {
-    const LogPlan pl = plan_of(p, ws, nullptr);
+    const LogPlan pl = plan_of(p, ws);
     return p.n_top == 0 ? launch_top<0>(p, pl, s) : p.n_top == 1 ? launch_top<1>(p, pl, s) : p.n_top <= 8 ? launch_top<8>(p, pl, s)
            : p.n_top <= 32 ? launch_top<32>(p, pl, s) : launch_top<64>(p, pl, s);
 }

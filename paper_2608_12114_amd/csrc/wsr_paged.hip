@@ -468,7 +468,7 @@ __global__ __launch_bounds__(JT) __attribute__((amdgpu_waves_per_eu(W == 1 ? 8 :
 /* Sequences times key heads below which units are few: one launch then pays up to 768 keys (one sequence of 500 11.7 us in
    two, 8.1 in one with twelve waves a unit; of 1000 11.5 and 11.8), and beyond it up to 1536 (63 of 1000 33.4 us in two, 31 in
    one; 64 of 500 25.8 and 18.5, with twelve waves a unit 19.7). */
-constexpr int FEW_UNITS = 256;
+constexpr int FEW_UNITS = 256, WHOLE = 768;
 /* Rows up to which a row's parts are joined by four waves: 32 rows of 86 parts 15 us by one wave each, so 6. */
 constexpr int FEW_ROWS = 2048;
 
@@ -487,13 +487,15 @@ static int64_t most_units(const wsr_paged& p, const PagedPlan& pl) {
     return p.n_kv_heads * (rows / pl.rows + std::min(p.n_seqs, p.n_tokens));
 }
 
+static int32_t held_of(int32_t rows, int32_t head_dim) { return 256 * (rows > 32 ? 2 : waves_of(head_dim, rows / 16)); }
+constexpr int SPARE = 64;                     /* slots, for what fp32 sums of lengths may be off by */
 static PagedPlan paged_plan(const wsr_paged& p) {
     PagedPlan pl{};
     pl.rows = tile_rows(p);
-    pl.held = 256 * (pl.rows > 32 ? 2 : waves_of(p.head_dim, pl.rows / 16));
-    /* parts come to what the chip holds where units are few, to twice that elsewhere, and what fp32 sums may be off by */
-    pl.slots = (most_units(p, pl) <= few_units(pl) ? 1 : 2) * pl.held + 64;
-    pl.whole = p.max_len <= ((int64_t)p.n_kv_heads * std::min(p.n_seqs, p.n_tokens) < FEW_UNITS ? 768 : 1536);
+    pl.held = held_of(pl.rows, p.head_dim);
+    /* parts come to what the chip holds where units are few, to twice that elsewhere */
+    pl.slots = (most_units(p, pl) <= few_units(pl) ? 1 : 2) * pl.held + SPARE;
+    pl.whole = p.max_len <= ((int64_t)p.n_kv_heads * std::min(p.n_seqs, p.n_tokens) < FEW_UNITS ? WHOLE : 2 * WHOLE);
     /* n / d = (n * M) >> (31 + s), 2^s >= d, M = 2^(31 + s) / d + 1, for n < 2^31: M d is over 2^(31 + s) by at most d */
     int s = 0;
     while ((int64_t)1 << s < p.cache.page_size) ++s;
@@ -502,9 +504,13 @@ static PagedPlan paged_plan(const wsr_paged& p) {
     return pl;
 }
 
+/* What the call needs, and any of fewer tokens, whose tiles may be smaller and more. */
 size_t paged_workspace(const wsr_paged& p) {
     const PagedPlan pl = paged_plan(p);
-    return pl.whole ? 256 : (size_t)pl.slots * pl.rows * (p.head_dim + 4) * sizeof(float);
+    if (p.max_len <= WHOLE) return 256;
+    size_t rows = (size_t)pl.slots * pl.rows;
+    for (int32_t r = 16; r < pl.rows; r *= 2) rows = std::max(rows, (size_t)(2 * held_of(r, p.head_dim) + SPARE) * r);
+    return rows * (p.head_dim + 4) * sizeof(float);
 }
 
 /* Workgroups of the first launch. */

@@ -173,3 +173,25 @@ def test_definitions_by_hand():
     assert (rank, top) == (2, [1, 0, 2, -1]) and logp == pytest.approx(math.log(0.25)) and entropy == pytest.approx(1.5 * math.log(2))
     assert top_logp[0] == pytest.approx(math.log(0.5)) and top_logp[3] == -math.inf
     assert su.logprobs64(row, 3, 0.0, 1) == (-math.inf, 3, 0.0, [1], [0.0]) and su.logprobs64(row, 4, 1.0, 0)[:2] == (-math.inf, -1)
+
+
+@pytest.mark.parametrize("D,heads,kv,seqs", [(64, 8, 8, 8), (64, 64, 8, 32), (128, 32, 8, 2), (128, 64, 8, 300), (256, 16, 2, 24), (128, 8, 1, 1)])
+@pytest.mark.parametrize("max_len", [100, 768, 1000, 1536, 1537, 1 << 20])
+def test_a_workspace_for_many_tokens_serves_fewer(D, heads, kv, seqs, max_len):
+    def need(tokens, n=seqs, **over):
+        return wsr.wsr_paged_workspace_bytes(_paged(_pages(page_size=64, max_pages=1 << 14), n_heads=heads, n_kv_heads=kv, head_dim=D,
+                                                    n_seqs=n, n_tokens=tokens, max_len=max_len, **over))
+
+    sizes = [need(t) for t in (*range(1, 70), *range(70, 3000, 37), 20000)]
+    assert sizes == sorted(sizes) and sizes[0] > 0
+    sizes = [need(n, n, starts=None) for n in range(1, 500)]
+    assert sizes == sorted(sizes)
+
+
+@pytest.mark.parametrize("vocab", [1000, 4097, 32000, 128256, 1 << 24])
+@pytest.mark.parametrize("n_top", [0, 1, 20, 64])
+def test_a_workspace_for_many_rows_serves_fewer(vocab, n_top):
+    sizes = [wsr.wsr_logprobs_workspace_bytes(_logprobs(vocab=vocab, n_rows=r, n_top=n_top)) for r in (*range(1, 800), 1000, 1536, 1537, 4000, 1 << 16)]
+    assert sizes == sorted(sizes) and sizes[0] > 0
+    fewer = [wsr.wsr_logprobs_workspace_bytes(_logprobs(vocab=vocab, n_rows=33, n_top=n)) for n in range(65)]
+    assert fewer == sorted(fewer)
