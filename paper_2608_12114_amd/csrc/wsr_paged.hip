@@ -473,7 +473,7 @@ constexpr int FEW_UNITS = 256, WHOLE = 768;
 constexpr int FEW_ROWS = 2048;
 
 /* Rows of a tile: as many as a sequence's fill, on average; 128 where there are tiles enough of them (a chunk of 512 tokens of
-   32 heads on 8, 128 tiles, 18.6 us with 128 rows and 15.5 with 64; two of up to 512 behind 4096, 216 tiles, 78 and 87). */
+   32 heads on 8, 128 tiles, 18.6 us with 128 rows and 15.5 with 64; two of up to 512 behind 4096, 216 tiles, 72 and 81). */
 static int tile_rows(const wsr_paged& p) {
     const int64_t rows = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads), n = p.n_seqs;
     if (rows <= 16 * n) return 16;
