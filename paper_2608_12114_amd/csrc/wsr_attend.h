@@ -30,7 +30,7 @@ __device__ __forceinline__ float lse_of(float m, float l, float scale) { return 
    alternate blocks of KT keys. */
 template <int FMT, int D, int RW>
 struct AttendBlocks {
-    static constexpr int KW = AW / RW, KT = KW == 1 ? 64 : 32, TILES = KT / 32;
+    static constexpr int KW = AW / RW, KT = KW == 1 && D < 256 ? 64 : 32, TILES = KT / 32;
     static constexpr int PIECES = D / 8;                        /* 16-byte pieces of a key */
     static constexpr int ROW = 2 * D;                           /* bytes of a key */
     static constexpr int HALF = KT * PIECES;                    /* pieces of a block of keys (and of values) */
@@ -46,9 +46,9 @@ struct AttendBlocks {
 
     /* Piece x of a key lies at x ^ swz: the 16 keys of a read of keys, and the four keys times four pieces of a
        transposing read of values, lie on the 64 banks once each (two keys of 64 share a round of banks). */
-    static __device__ __forceinline__ int kswz(int key) { return D == 128 ? key & 15 : key >> 1 & 7; }
+    static __device__ __forceinline__ int kswz(int key) { return D >= 128 ? key & 15 : key >> 1 & 7; }
     static __device__ __forceinline__ int vswz(int key) {
-        return D == 128 ? (key & 3) << 2 | (key >> 2 & 1) : (key >> 1 & 1) << 2 | (key >> 2 & 1);
+        return D >= 128 ? (key & 3) << 2 | (key >> 2 & 1) : (key >> 1 & 1) << 2 | (key >> 2 & 1);
     }
 
     /* Places relative to the first group's first buffer, `base` bytes on for the wave's own group. */

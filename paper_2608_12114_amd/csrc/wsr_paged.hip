@@ -473,12 +473,14 @@ constexpr int FEW_UNITS = 256, WHOLE = 768;
 constexpr int FEW_ROWS = 2048;
 
 /* Rows of a tile: as many as a sequence's fill, on average; 128 where there are tiles enough of them (a chunk of 512 tokens of
-   32 heads on 8, 128 tiles, 18.6 us with 128 rows and 15.5 with 64; two of up to 512 behind 4096, 216 tiles, 72 and 81). */
+   32 heads on 8, 128 tiles, 18.6 us with 128 rows and 15.5 with 64; two of up to 512 behind 4096, 216 tiles, 72 and 81), of
+   heads of 256, whose workgroups are one to a CU, half as many (16 on 4: 4 chunks of up to 64, 32 tiles, 43 and 30; two of up to
+   512 behind 4096, 108 tiles, 87 and 112, with 32 rows 173). */
 static int tile_rows(const wsr_paged& p) {
     const int64_t rows = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads), n = p.n_seqs;
     if (rows <= 16 * n) return 16;
-    if (rows <= 32 * n || p.head_dim == 256) return 32;
-    return rows <= 64 * n || p.n_kv_heads * (rows / 128) < 160 ? 64 : 128;
+    if (rows <= 32 * n) return 32;
+    return rows <= 64 * n || p.n_kv_heads * (rows / 128) < (p.head_dim == 256 ? 80 : 160) ? 64 : 128;
 }
 
 /* Units of a call, at most. */
@@ -487,7 +489,7 @@ static int64_t most_units(const wsr_paged& p, const PagedPlan& pl) {
     return p.n_kv_heads * (rows / pl.rows + std::min(p.n_seqs, p.n_tokens));
 }
 
-static int32_t held_of(int32_t rows, int32_t head_dim) { return 256 * (rows > 32 ? 2 : waves_of(head_dim, rows / 16)); }
+static int32_t held_of(int32_t rows, int32_t head_dim) { return 256 * (rows <= 32 ? waves_of(head_dim, rows / 16) : head_dim == 256 ? 1 : 2); }
 constexpr int SPARE = 64;                     /* slots, for what fp32 sums of lengths may be off by */
 static PagedPlan paged_plan(const wsr_paged& p) {
     PagedPlan pl{};

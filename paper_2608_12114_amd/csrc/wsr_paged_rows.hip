@@ -4,7 +4,8 @@
  * A workgroup takes a tile of 64 or 128 rows, 32 to a wave, so that a block of keys and values that is fetched into LDS once
  * serves all of them; wsr_attend.h does the rest.  Blocks alternate between two buffers, one fetched while the other is
  * worked on: a lane knows the place of one key, the places of the pieces that it fetches come from the other lanes, and
- * the pages of the block after it are looked up meanwhile.
+ * the pages of the block after it are looked up meanwhile.  Heads of 256 have blocks of 32 keys and one workgroup a CU: 2 chunks
+ * of up to 512 tokens behind 4096, 16 heads on 4, 88 us (in tiles of 32 rows, eight times the reads, 173).
  *
  * Chunks of prompts are bound by the matrix cores and the exponentials between their products, as attention behind a prefix
  * is: 2 chunks of up to 512 tokens behind 4096, 32 heads on 8, 39 GFLOP, 72 us with the join (61 without, 640 TFLOP/s).  Drafts
@@ -105,7 +106,7 @@ struct PagedBlocks : wsr_step::AttendBlocks<FMT, D, RW> {
 };
 
 template <int FMT, int D, int RW, bool ONCE>
-__global__ __launch_bounds__(AT) __attribute__((amdgpu_waves_per_eu(2))) void k_paged_rows(wsr_paged p, PagedPlan pl) {
+__global__ __launch_bounds__(AT) __attribute__((amdgpu_waves_per_eu(D == 256 ? 1 : 2))) void k_paged_rows(wsr_paged p, PagedPlan pl) {
     typedef PagedBlocks<FMT, D, RW, ONCE> A;
     __shared__ u32x4 lds_room[A::LDS];
     l_char* lds = (l_char*)lds_room;
@@ -214,10 +215,15 @@ static hipError_t launch_dim(const wsr_paged& p, const PagedPlan& pl, int rw, bo
     return hipGetLastError();
 }
 
+template <int FMT>
+static hipError_t launch_fmt(const wsr_paged& p, const PagedPlan& pl, int rw, bool once, int64_t blocks, hipStream_t s) {
+    return p.head_dim == 64    ? launch_dim<FMT, 64>(p, pl, rw, once, blocks, s)
+           : p.head_dim == 128 ? launch_dim<FMT, 128>(p, pl, rw, once, blocks, s)
+                               : launch_dim<FMT, 256>(p, pl, rw, once, blocks, s);
+}
+
 hipError_t launch_paged_rows(const wsr_paged& p, const PagedPlan& pl, int rw, bool once, int64_t blocks, hipStream_t s) {
-    if (p.fmt == WSR_F16)
-        return p.head_dim == 64 ? launch_dim<WSR_F16, 64>(p, pl, rw, once, blocks, s) : launch_dim<WSR_F16, 128>(p, pl, rw, once, blocks, s);
-    return p.head_dim == 64 ? launch_dim<WSR_BF16, 64>(p, pl, rw, once, blocks, s) : launch_dim<WSR_BF16, 128>(p, pl, rw, once, blocks, s);
+    return p.fmt == WSR_F16 ? launch_fmt<WSR_F16>(p, pl, rw, once, blocks, s) : launch_fmt<WSR_BF16>(p, pl, rw, once, blocks, s);
 }
 
 }  // namespace wsr_serve

@@ -97,3 +97,43 @@ def test_as_many_parts_as_there_is_room_for(N, seqs, n, room):
     c = Case([n] * seqs, [2048] * seqs, 8 * N, N, 64, F16, page=32, room=room)
     c.run()
     c.check()
+
+
+MANY = 64, 8                                  # heads: enough tiles of 128 rows, from some 120 tokens on
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("n,lens", [(120, 130), (121, 900), (150, 2900)])
+def test_tiles_of_most_rows(D, n, lens):
+    """128 rows, in one part and in several; of unequal sequences, whose last tiles are part empty."""
+    c = Case([n, n - 3, n + 1], [lens, n - 3, lens + 77], *MANY, D, (F16, BF16)[n % 2], page=20, seed=n)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("page", [1, 19])
+def test_holes_in_tiles_of_most_rows(D, page):
+    n, lens = 121, 1000
+    holes = [((0, i), (-1, 1 << 30)[i % 2]) for i in range(lens // page) if i * page % 256 < 100] + [((1, i), -7) for i in range(-(-(lens + 50) // page))]
+    c = Case([n, n, n], [lens, lens + 50, n // 2], *MANY, D, F16, page=page, holes=holes)
+    c.run()
+    c.check()
+    assert torch.isneginf(c.lse[n:2 * n]).all()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("value", [INF, NAN])
+def test_broken_values_in_tiles_of_most_rows(D, value):
+    n, lens = 170, 800
+    c = Case([n, n], [lens, n], *MANY, D, F16, page=8)
+    place = lens - n // 2
+    at = int(c.table[0, place // 8]), place % 8, 3, 5
+    c.v[at] = value
+    c.run()
+    hit = torch.zeros_like(c.out, dtype=torch.bool)
+    hit[n - n // 2:n, 24:32, 5] = True
+    assert (torch.isnan(c.out[hit]) if value != value else c.out[hit] == value).all()
+    c.v[at] = 0.0
+    out, _, bound, _ = su.paged64(c.q, c.k, c.v, c.table, 8, c.starts, c.lens, c.max_len, c.scale)
+    assert ((c.out.double() - out).abs()[~hit] <= bound[~hit]).all()
