@@ -12,7 +12,7 @@
  * The n largest: a wave keeps its best 64 in order, one per lane, as 64-bit keys (the logit's bits in an order of whole
  * numbers, then the index from the top, so that equal logits go by index).  Logits that pass the n-th key, which after
  * the first few hundred are rare, are collected in LDS and merged in 64 at a time, sorted by compare-and-swap networks
- * over the wave.  The first chunk's threshold is the n-th largest of the lanes' maxima, which n logits reach.  A single
+ * over the wave.  The first chunks' threshold is the n-th largest of the lanes' maxima, which n logits reach.  A single
  * alternative is a lane's largest and needs none of this.
  *
  * Bound by HBM where rows are many: 2055 rows of 50257, 413 MB, 70 to 72 us without alternatives (5.8 TB/s; eleven
@@ -339,12 +339,13 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_
                         if (v[u][j] > one) one = v[u][j], one_at = i0 + u * LT * 4 + j;
         }
         if constexpr (TOP > 1) {
-            if (c == begin) {
-                const int order = __builtin_bit_cast(int, sorted<WAVE>(top, true, lane));
+            /* again for the second chunk: 1461 rows of 32000 with 21 46.3 us, so 44.9; for the third too, no less */
+            if (c < begin + 2) {
+                const int order = __builtin_bit_cast(int, sorted<WAVE>(m, true, lane));
                 const float bar = __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, p.n_top - 1));
                 if (bar > NEG_INF) b.raise(key_of(bar, -1));
                 if (lane == 0) quarter[wave] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, fourth));
-                __syncthreads();
+                if (c == begin) __syncthreads();
             }
             /* four waves that have seen n / 4 logits of at least this: no smaller one is among the workgroup's n */
             float common = quarter[0];
