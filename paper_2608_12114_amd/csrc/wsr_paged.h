@@ -128,7 +128,8 @@ __device__ __forceinline__ bool find(const wsr_paged& p, const PagedPlan& pl, in
         if (per == 1) {
             o.s = Seq{of(s.t0), of(s.n), of(s.len), of(s.rows), of(s.tiles)};
             o.seq = lo + w, o.parts = of(parts), o.at = item - items, o.slot = slots;
-            return true;
+            /* starts that decrease may count more than 32 bits hold */
+            return by_seq || (o.at >= 0 && (int64_t)(o.s.tiles * N) * o.parts > o.at);
         }
         lo += w * per, n = min(per, n - w * per);
     }

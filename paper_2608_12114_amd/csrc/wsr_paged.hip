@@ -365,7 +365,7 @@ __global__ __launch_bounds__(NW * WAVE) __attribute__((amdgpu_waves_per_eu(waves
             if (p.lse && wave == 0 && g == 0) p.lse[(int64_t)tok * p.n_heads + qh] = lse_of(m, l, p.scale);
         } else {
             const int slot = at_place.slot + at_place.at;
-            if (slot >= pl.slots) continue;
+            if ((uint32_t)slot >= (uint32_t)pl.slots) continue;
             float* to = pl.part + ((int64_t)slot * R + row - row0) * (D + 4);
 #pragma unroll
             for (int i = 0; i < PER; ++i) *(f4_t*)(to + 16 * (wave + NW * i) + 4 * g) = sum[i];
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(JT) __attribute__((amdgpu_waves_per_eu(W == 1 ? 8 :
         Place o_place;
         if (b < 0 || !find(p, pl, b, true, o_place) || o_place.parts == 1 || t != tok) continue;
         const int row = (tok - o_place.s.t0) * G + qh % G, slot = o_place.slot + (row / R * p.n_kv_heads + qh / G) * o_place.parts;
-        if (slot < 0 || slot + o_place.parts > pl.slots) continue;
+        if (slot < 0 || slot > pl.slots - o_place.parts) continue;
         parts = o_place.parts;
         from = pl.part + ((int64_t)slot * R + row % R) * (D + 4);
     }

@@ -195,7 +195,7 @@ __global__ __launch_bounds__(AT) __attribute__((amdgpu_waves_per_eu(D == 256 ? 1
         if (p.lse && h == 0) p.lse[(int64_t)tok * p.n_heads + qh] = lse_of(a.m, a.l, p.scale);
     } else {
         const int to_slot = place.slot + (tile * N + head) * parts + part;
-        if (to_slot >= pl.slots) return;
+        if ((uint32_t)to_slot >= (uint32_t)pl.slots) return;
         float* w = pl.part + ((int64_t)to_slot * R + row - row0) * (D + 4);
 #pragma unroll
         for (int i = 0; i < A::DT; ++i)

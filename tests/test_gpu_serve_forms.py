@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import serve_util as su
-from gpu_util import needs_gpu
+from gpu_util import needs_gpu, stream
+from paper_2608_12114_amd import wsr
 from test_gpu_serve_paged import BF16, F16, INF, NAN, Case
 
 pytestmark = [pytest.mark.gpu, needs_gpu]
@@ -137,3 +138,26 @@ def test_broken_values_in_tiles_of_most_rows(D, value):
     c.v[at] = 0.0
     out, _, bound, _ = su.paged64(c.q, c.k, c.v, c.table, 8, c.starts, c.lens, c.max_len, c.scale)
     assert ((c.out.double() - out).abs()[~hit] <= bound[~hit]).all()
+
+
+@pytest.mark.parametrize("H,N,D,n", [(8, 2, 64, 1), (8, 8, 128, 1), (64, 8, 128, 3), (64, 2, 64, 40), (16, 2, 256, 12)])
+@pytest.mark.parametrize("room", [0, 3000])
+def test_anything_on_the_device_stays_inside(H, N, D, n, room):
+    """Starts that fall, lengths and pages of any value: whatever comes out, nothing around the outputs is touched."""
+    seqs = 300 if n == 1 else 70
+    c = Case([n] * seqs, [n + 20] * seqs, H, N, D, F16, page=24, room=room)
+    c.k.fill_(0.5), c.v.fill_(0.25)
+    g = torch.Generator().manual_seed(H * D + n)
+    any32 = lambda t, lo=-2 ** 31, hi=2 ** 31 - 1: t.copy_(torch.randint(lo, hi, t.shape, generator=g))  # noqa: E731
+    T, edge = n * seqs, 50
+    wide, wide_lse = c.out.new_full((T + 2 * edge, H, D), 77.0), c.lse.new_full((T + 2 * edge, H), 77.0)
+    ws = torch.full((wsr.wsr_paged_workspace_bytes(wsr.make_paged(**c.fields)) + (2 << 20),), 255, dtype=torch.uint8, device="cuda")
+    for starts in ((-5, T + 5), (0, T + 1), (-2 ** 31, 2 ** 31 - 1), (T, T + 1)):
+        any32(c.dev_starts, *starts), any32(c.dev_lens), any32(c.table)
+        c.table[:, ::2] = torch.randint(0, c.k.shape[0], c.table[:, ::2].shape, generator=g).to(c.table)
+        p = wsr.make_paged(**{**c.fields, "out": wide[edge:], "lse": wide_lse[edge:]})
+        wsr.wsr_paged_attention(p, ws[1 << 20:], ws.numel() - (2 << 20), stream())
+        torch.cuda.synchronize()
+        for t in (wide, wide_lse):
+            assert (t[:edge] == 77.0).all() and (t[-edge:] == 77.0).all()
+        assert (ws[:1 << 20] == 255).all() and (ws[-(1 << 20):] == 255).all()
