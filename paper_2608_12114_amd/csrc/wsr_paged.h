@@ -53,17 +53,16 @@ struct Sums {
     }
 };
 struct Cut {
-    float part, up;                           /* keys of a part; what is added before the number of parts is rounded down */
+    float inv, up;                            /* one over the keys of a part; what is added before the number of parts is rounded down */
 };
 __host__ __device__ __forceinline__ float few_units(const PagedPlan& pl) { return (float)pl.held * (pl.rows > 32 ? 0.5f : 0.125f); }
-__device__ __forceinline__ Cut cut_of(const PagedPlan& pl, const Sums& s) {
-    const float held = (float)pl.held, least = (float)(192 + 4 * pl.rows);
-    return s.units <= few_units(pl) ? Cut{fmaxf(least, s.keys / (held - s.units)), 0.999f}
-                                    : Cut{fmaxf(least, s.keys / (held * 2.f)), 0.f};
+/* Parts of the keys over `share`, where that is enough for one. */
+__device__ __forceinline__ Cut cut_by(const PagedPlan& pl, float inv_keys, float share, float up) {
+    return Cut{fminf(__builtin_amdgcn_rcpf((float)(192 + 4 * pl.rows)), share * inv_keys), up};
 }
 /* Parts of each of a sequence's units. */
 __device__ __forceinline__ int parts_of(const Seq& s, Cut cut) {
-    return (int)fminf(fmaxf(floorf((float)s.len / cut.part + cut.up), 1.f), 2048.f);
+    return (int)fminf(fmaxf(floorf(fmaf((float)s.len, cut.inv, cut.up)), 1.f), 2048.f);
 }
 
 /* The lanes' sums of themselves and those below: inside 16-lane rows, then the rows' last lanes handed on. */
@@ -99,7 +98,24 @@ __device__ __forceinline__ bool find(const wsr_paged& p, const PagedPlan& pl, in
 #pragma unroll 4
         for (int b = WAVE; b < p.n_seqs; b += WAVE) sums.add(seq_in(b + lane, 0, p.n_seqs), N);
         sums.keys = wsr::wave_sum(sums.keys), sums.units = wsr::wave_sum(sums.units);
-        cut = cut_of(pl, sums);
+        const float inv_keys = __builtin_amdgcn_rcpf(sums.keys), held = (float)pl.held;
+        if (sums.units <= few_units(pl)) {
+            float share = held - sums.units, by = sums.units * 0.5f;
+            cut = cut_by(pl, inv_keys, share, 0.999f);
+            if (p.n_seqs >= 8 && p.n_seqs <= WAVE) {
+                /* a sequence's last part is rounded up by half of one, not by one: in four tries the shortest parts that the
+                   chip holds at once (24 sequences of 5 drafts 66.7 us, so 63.3; where sequences are fewer, nothing) */
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i, by *= 0.5f) {
+                    const Cut next = cut_by(pl, inv_keys, share + by, 0.999f);
+                    const int all = __builtin_amdgcn_readlane(scan32(s.tiles * N * parts_of(s, next)), WAVE - 1);
+                    if (next.inv == cut.inv) break;
+                    if (all <= pl.held) cut = next, share += by;
+                }
+            }
+        } else {
+            cut = cut_by(pl, inv_keys, held * 2.f, 0.f);
+        }
     }
     int lo = 0, n = p.n_seqs;                 /* the sequences left, and items and slots of those before them */
     int items = 0, slots = 0;
