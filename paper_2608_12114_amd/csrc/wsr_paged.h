@@ -40,7 +40,7 @@ __device__ __forceinline__ Seq seq_at(const wsr_paged& p, int R, int b) {
 
 /* Where units are few against the workgroups that the chip holds, an eighth of them, or half for tiles of more than 32 rows,
    they are cut into as many parts as fill it once, the shorter ones rounded up (7 sequences of up to 65536 keys 257 us in a
-   graph, in one and a half rounds 267; 24 of 5 drafts of 8 heads 67, by the other rule 74).  Otherwise parts are half of what
+   graph, in one and a half rounds 267; 24 of 5 drafts of 8 heads 63, by the other rule 74).  Otherwise parts are half of what
    falls to a workgroup, and units of less than two such stay whole, so that whoever is done early takes another (16 sequences
    of 2000 with 32 key heads 58 us, by the first rule 67; 32 of up to 4096 63, with parts two thirds or four thirds as long 65).
    A part has 256 keys or more, of 64 (128) rows 448 (704), since its rows have to be written and read again.  Sums of lengths

@@ -9,8 +9,8 @@
  *
  * Chunks of prompts are bound by the matrix cores and the exponentials between their products, as attention behind a prefix
  * is: 2 chunks of up to 512 tokens behind 4096, 32 heads on 8, 39 GFLOP, 72 us with the join (61 without, 640 TFLOP/s).  Drafts
- * by the loads, one block in flight for each workgroup: 24 sequences of 5 with up to 6001 keys, 64 heads on 8, 280 MB, 66 us with
- * the join (58 without, 4.8 TB/s), without the hint that a tile that holds all of a sequence's rows is read once 74.
+ * by the loads, one block in flight for each workgroup: 24 sequences of 5 with up to 6001 keys, 64 heads on 8, 280 MB, 63 us with
+ * the join (54 without, 5.2 TB/s), without the hint that a tile that holds all of a sequence's rows is read once 70.
  */
 #include <hip/hip_runtime.h>
 
