@@ -101,9 +101,10 @@ wsr_status wsr_append_qkv(const wsr_qkv* p, void* stream);
    [0, max_len]; max_len <= max_pages * page_size.  n_tokens and n_seqs at most 2^20, n_heads at most 4096, tokens
    times heads at most 2^25; n_kv_heads * (n_seqs + a key head's rows / 16) past 2^23 may be refused.  head_dim 64, 128
    or 256; every pointer 16-byte aligned and every stride a multiple of 16 (of 4 for table, starts, lens and lse); lse
-   (n_tokens, n_heads) or null; out and lse overlap nothing.  ws: wsr_paged_workspace_bytes(), 256-byte aligned; what
-   it gives serves calls of fewer tokens too where the rest is the same (without starts, of fewer sequences).  Sums of probabilities, relative to within 2^8 of
-   the largest, times values are infinite past fp32's range. */
+   (n_tokens, n_heads) or null; out and lse overlap nothing.  Sums of probabilities, relative to within 2^8 of the largest,
+   times values are infinite past fp32's range.
+   ws: wsr_paged_workspace_bytes(), 256-byte aligned; what it gives serves calls of fewer tokens too where the rest is the
+   same (without starts, of fewer sequences). */
 typedef struct wsr_paged {
     int32_t fmt, n_heads, n_kv_heads, head_dim, n_seqs, n_tokens;
     float scale;
