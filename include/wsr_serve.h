@@ -55,7 +55,8 @@ typedef struct wsr_pages {
      pair j < rot_dim / 2, (a, b) = u at (j, j + rot_dim / 2), or WSR_QKV_PAIRS at (2 j, 2 j + 1), queries and keys:
                      (a cos t - b sin t, b cos t + a sin t),  t = positions[axis_of[j]][token] * freqs[j]
    Values from rot_dim on pass, and the value heads whole.  Queries are stored to q_out, keys and values to their place
-   in the cache, each rounded once to `fmt`; arithmetic is fp32, angles and their reduction 64 bits.
+   in the cache, each rounded once to `fmt`; arithmetic is fp32, angles are exact and reduced to a part of a turn right to 2^-50
+   while they come to less than 2^45, so that a position of 2^31 turns as exactly as one of 1.
    positions: device int32 (n_axes, n_tokens), or null: the token's place (n_axes 1).  axis_of: device int32
    [rot_dim / 2], clamped to [0, n_axes), or null (all 0).  freqs: device fp32 [rot_dim / 2].
    Tokens of no sequence, and places below 0, past the table's row or in holes, are not stored, and nothing else is

@@ -8,8 +8,8 @@
  * or two heads at a time.  A lane's values are two runs of four: j .. j + 3 and, rot_dim / 2 on, the other halves of
  * their pairs; past rot_dim, or where pairs stand side by side, eight in a row.  A norm is a sum over the head's lanes.
  * The sine and cosine of a lane's four angles are the same for all heads and taken once per wave: position times
- * frequency in 64 bits (of 31 and 24), reduced to a part of a turn there, so that far positions lose nothing before that
- * part becomes fp32.
+ * frequency (of 31 and 24 bits, 55 in all) as a sum of two 64-bit numbers, reduced to a part of a turn by a 2 / pi of two
+ * more, so that far positions lose nothing before that part becomes fp32.
  *
  * Bound by HBM for prompts: 6300 tokens of 48 heads of 128, 241 MB, 49 us, 4.9 TB/s (a copy of 1 GiB 4.8), by a launch and one
  * chain of loads for few tokens: one token 4.1 us in a graph, 64 of 80 heads 5.2.
@@ -36,10 +36,14 @@ __device__ __forceinline__ float head_sum(float v) {
 }
 
 /* Sine and cosine of an angle: whole quarter turns and a rest of at most pi / 4 in 64 bits, of which the series up to x^9 and
-   x^8 leave 2^-29 and 2^-25 (0.1 to 0.2 us less than a general function: 1 token of 32 heads on 8 4.2 us, so 4.06). */
-__device__ __forceinline__ void turn_of(double angle, float& si, float& co) {
-    const double quarters = angle * 0.63661977236758134, whole = rint(quarters);    /* 2 / pi */
-    const float x = (float)(quarters - whole) * 1.5707963267948966f, y = x * x;
+   x^8 leave 2^-29 and 2^-25 (0.1 to 0.2 us less than a general function: 1 token of 32 heads on 8 4.2 us, so 4.06).  What the
+   product and 2 / pi lose to 64 bits, up to 2^-22 of a quarter at positions of 2^31, is added to the rest, which is then right
+   to 2^-53 while there are fewer than 2^45 quarters. */
+__device__ __forceinline__ void turn_of(double position, double frequency, float& si, float& co) {
+    constexpr double PER = 0.63661977236758134, PER_LOW = -3.9357353350364972e-17;     /* 2 / pi */
+    const double angle = position * frequency, low = fma(position, frequency, -angle);
+    const double whole = rint(angle * PER), rest = fma(angle, PER, -whole) + fma(low, PER, angle * PER_LOW);
+    const float x = (float)rest * 1.5707963267948966f, y = x * x;
     const int n = (int)(whole - 4.0 * floor(whole * 0.25));
     const float s = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), x);
     const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, 1.f / 40320.f, -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
@@ -106,7 +110,7 @@ __global__ __launch_bounds__(PT) void k_append(wsr_qkv p, Steps st, int64_t firs
     for (int i = 0; i < 4; ++i) {
         co[i] = 1.f, si[i] = 0.f;
         if (!turned) continue;
-        turn_of((p.positions ? (double)pos[i] : (double)place) * (double)freq[i], si[i], co[i]);
+        turn_of(p.positions ? (double)pos[i] : (double)place, (double)freq[i], si[i], co[i]);
     }
 
 #pragma unroll 1
