@@ -1,5 +1,10 @@
 /*
  * wsr_paged.h - how the work of paged attention is cut: units, their parts, and the slots those leave their results in.
+ *
+ * Items are the parts of all units, sequence after sequence.  Where sequences are few, every wave finds its item by sums over
+ * all of them, a lane to each of 64 at a time.  The reads of all workgroups grow with the square of the sequences there (2^20 of
+ * them would take minutes), so where they are many one workgroup writes the sums up to each sequence first (k_paged_line) and a
+ * wave searches those, 64 ways a step.
  */
 #ifndef WSR_PAGED_H
 #define WSR_PAGED_H
@@ -7,6 +12,18 @@
 #include "wsr_serve_device.h"
 
 namespace wsr_serve {
+
+struct Cut {
+    float inv, up;                            /* one over the keys of a part; what is added before the number of parts is rounded down */
+};
+struct Upto {
+    int32_t items, slots;                     /* of the sequences before one, LINE_END at most */
+};
+constexpr int32_t LINE_END = 1 << 30;         /* more than a launch has workgroups */
+struct Line {
+    Cut cut;
+    Upto upto[1];                             /* [n_seqs] */
+};
 
 struct PagedPlan {
     int32_t rows;                             /* R, rows of a tile */
@@ -16,6 +33,7 @@ struct PagedPlan {
     int32_t shift;                            /* division by page_size: (n * magic) >> shift for n < 2^31 */
     uint64_t magic;
     float* part;                              /* [slots][R][head_dim + 4] */
+    Line* line;                               /* of many sequences, as k_paged_line leaves it; else null */
 };
 
 /* ---- units and their parts -------------------------------------------------------------------------- */
@@ -52,13 +70,15 @@ struct Sums {
         units += of, keys = fmaf(of, (float)s.len, keys);
     }
 };
-struct Cut {
-    float inv, up;                            /* one over the keys of a part; what is added before the number of parts is rounded down */
-};
 __host__ __device__ __forceinline__ float few_units(const PagedPlan& pl) { return (float)pl.held * (pl.rows > 32 ? 0.5f : 0.125f); }
 /* Parts of the keys over `share`, where that is enough for one. */
 __device__ __forceinline__ Cut cut_by(const PagedPlan& pl, float inv_keys, float share, float up) {
     return Cut{fminf(__builtin_amdgcn_rcpf((float)(192 + 4 * pl.rows)), share * inv_keys), up};
+}
+/* The cut by sums over all sequences; where units are few, as it is before any tries. */
+__device__ __forceinline__ Cut cut_of(const PagedPlan& pl, const Sums& sums) {
+    const float inv_keys = __builtin_amdgcn_rcpf(sums.keys), held = (float)pl.held;
+    return sums.units <= few_units(pl) ? cut_by(pl, inv_keys, held - sums.units, 0.999f) : cut_by(pl, inv_keys, held * 2.f, 0.f);
 }
 /* Parts of each of a sequence's units. */
 __device__ __forceinline__ int parts_of(const Seq& s, Cut cut) {
@@ -80,6 +100,22 @@ struct Place {
     Seq s;
     int seq, at, parts, slot;                 /* at: item of the sequence; slot: of the sequence's first part */
 };
+/* find() by the sums up to each sequence: the last one that no more than `item` items lie before. */
+__device__ __forceinline__ bool find_upto(const wsr_paged& p, const PagedPlan& pl, int item, bool by_seq, Place& o) {
+    const int lane = threadIdx.x % WAVE;
+    int b = by_seq ? item : 0;
+    for (int n = by_seq ? 1 : p.n_seqs; n > 1;) {               /* among b .. b + n - 1, and none lies before b */
+        const int step = (n + WAVE - 1) / WAVE, at = lane * step;
+        const int c = __builtin_popcountll(__ballot(at < n && pl.line->upto[b + min(at, n - 1)].items <= item));
+        b += (c - 1) * step, n = min(step, n - (c - 1) * step);
+    }
+    auto of = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    b = of(b);
+    const Seq s = seq_at(p, pl.rows, b);
+    o.s = Seq{of(s.t0), of(s.n), of(s.len), of(s.rows), of(s.tiles)};
+    o.seq = b, o.parts = pl.whole ? 1 : of(parts_of(s, pl.line->cut)), o.at = item - of(pl.line->upto[b].items), o.slot = of(pl.line->upto[b].slots);
+    return by_seq || (o.at >= 0 && (int64_t)(o.s.tiles * p.n_kv_heads) * o.parts > o.at);
+}
 /* Item `item` of the call, or (by_seq) the first of sequence `item`: its sequence, how that is cut and where its parts lie.
    False where there is no such item. */
 __device__ __forceinline__ bool find(const wsr_paged& p, const PagedPlan& pl, int item, bool by_seq, Place& o) {
@@ -90,7 +126,8 @@ __device__ __forceinline__ bool find(const wsr_paged& p, const PagedPlan& pl, in
         if (b >= n) s.rows = s.tiles = s.n = s.len = 0;
         return s;
     };
-    Seq s = seq_in(lane, 0, p.n_seqs);
+    Seq s = seq_in(lane, 0, p.n_seqs);        /* on its way before the branch: one sequence of 500 8.2 us, behind it 8.4 */
+    if (pl.line) return find_upto(p, pl, item, by_seq, o);
     Cut cut{1.f, 0.f};
     if (!pl.whole) {
         Sums sums{0.f, 0.f};
@@ -98,23 +135,19 @@ __device__ __forceinline__ bool find(const wsr_paged& p, const PagedPlan& pl, in
 #pragma unroll 4
         for (int b = WAVE; b < p.n_seqs; b += WAVE) sums.add(seq_in(b + lane, 0, p.n_seqs), N);
         sums.keys = wsr::wave_sum(sums.keys), sums.units = wsr::wave_sum(sums.units);
-        const float inv_keys = __builtin_amdgcn_rcpf(sums.keys), held = (float)pl.held;
-        if (sums.units <= few_units(pl)) {
-            float share = held - sums.units, by = sums.units * 0.5f;
-            cut = cut_by(pl, inv_keys, share, 0.999f);
-            if (p.n_seqs >= 8 && p.n_seqs <= WAVE) {
-                /* a sequence's last part is rounded up by half of one, not by one: in four tries the shortest parts that the
-                   chip holds at once (24 sequences of 5 drafts 66.7 us, so 63.3; where sequences are fewer, nothing) */
+        cut = cut_of(pl, sums);
+        if (sums.units <= few_units(pl) && p.n_seqs >= 8 && p.n_seqs <= WAVE) {
+            /* a sequence's last part is rounded up by half of one, not by one: in four tries the shortest parts that the
+               chip holds at once (24 sequences of 5 drafts 66.7 us, so 63.3; where sequences are fewer, nothing) */
+            const float inv_keys = __builtin_amdgcn_rcpf(sums.keys);
+            float share = (float)pl.held - sums.units, by = sums.units * 0.5f;
 #pragma unroll 1
-                for (int i = 0; i < 4; ++i, by *= 0.5f) {
-                    const Cut next = cut_by(pl, inv_keys, share + by, 0.999f);
-                    const int all = __builtin_amdgcn_readlane(scan32(s.tiles * N * parts_of(s, next)), WAVE - 1);
-                    if (next.inv == cut.inv) break;
-                    if (all <= pl.held) cut = next, share += by;
-                }
+            for (int i = 0; i < 4; ++i, by *= 0.5f) {
+                const Cut next = cut_by(pl, inv_keys, share + by, 0.999f);
+                const int all = __builtin_amdgcn_readlane(scan32(s.tiles * N * parts_of(s, next)), WAVE - 1);
+                if (next.inv == cut.inv) break;
+                if (all <= pl.held) cut = next, share += by;
             }
-        } else {
-            cut = cut_by(pl, inv_keys, held * 2.f, 0.f);
         }
     }
     int lo = 0, n = p.n_seqs;                 /* the sequences left, and items and slots of those before them */

@@ -374,6 +374,46 @@ __global__ __launch_bounds__(NW * WAVE) __attribute__((amdgpu_waves_per_eu(waves
     }
 }
 
+/* The cut, and the items and slots before each sequence, by one workgroup, a lane to each of 1024 sequences at a time.  Starts
+   that fall may count more items than 32 bits hold; sums then stay at LINE_END. */
+constexpr int NT = 1024, NW = NT / WAVE;
+__global__ __launch_bounds__(NT) void k_paged_line(wsr_paged p, PagedPlan pl) {
+    __shared__ float keys[NW], units[NW];
+    __shared__ int64_t all[2][NW], cuts[2][NW];                 /* of the waves, of this round and the one before */
+    const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), N = p.n_kv_heads;
+    Cut cut{1.f, 0.f};
+    if (!pl.whole) {
+        Sums sums{0.f, 0.f};
+#pragma unroll 4
+        for (int b = threadIdx.x; b < p.n_seqs; b += NT) sums.add(seq_at(p, pl.rows, b), N);
+        sums.keys = wsr::wave_sum(sums.keys), sums.units = wsr::wave_sum(sums.units);
+        if (lane == 0) keys[wave] = sums.keys, units[wave] = sums.units;
+        __syncthreads();
+        sums = Sums{0.f, 0.f};
+        for (int w = 0; w < NW; ++w) sums.keys += keys[w], sums.units += units[w];
+        cut = cut_of(pl, sums);
+        if (threadIdx.x == 0) pl.line->cut = cut;
+    }
+    int64_t items = 0, slots = 0;
+    Seq next = seq_at(p, pl.rows, min((int)threadIdx.x, p.n_seqs - 1));
+    for (int b0 = 0, odd = 0; b0 < p.n_seqs; b0 += NT, odd ^= 1) {
+        const Seq s = next;
+        const int b = b0 + threadIdx.x;
+        if (b0 + NT < p.n_seqs) next = seq_at(p, pl.rows, min(b + NT, p.n_seqs - 1));
+        const int parts = pl.whole ? 1 : parts_of(s, cut);
+        const int mine = b < p.n_seqs ? (int)min((int64_t)(s.tiles * N) * parts, (int64_t)LINE_END / WAVE) : 0, cutting = parts > 1 ? mine : 0;
+        const int to = scan32(mine), cuts_to = scan32(cutting);
+        if (lane == WAVE - 1) all[odd][wave] = to, cuts[odd][wave] = cuts_to;
+        __syncthreads();
+        int64_t i = items + to - mine, c = slots + cuts_to - cutting;
+        for (int w = 0; w < NW; ++w) {
+            if (w < wave) i += all[odd][w], c += cuts[odd][w];
+            items += all[odd][w], slots += cuts[odd][w];
+        }
+        if (b < p.n_seqs) pl.line->upto[b] = Upto{(int32_t)min(i, (int64_t)LINE_END), (int32_t)min(c, (int64_t)LINE_END)};
+    }
+}
+
 /* Rows whose unit is cut.  A part's row takes D / 4 lanes: where rows are many, W = 1, a wave has a row in each of its groups of
    so many lanes (2 chunks of up to 512 tokens 11 us, with one row a wave 16); where they are few, four waves take the parts
    of one row, a group each.  AHEAD parts are loaded at a time. */
@@ -472,6 +512,16 @@ constexpr int FEW_UNITS = 256, WHOLE = 768;
 /* Rows up to which a row's parts are joined by four waves: 32 rows of 86 parts 15 us by one wave each, so 6. */
 constexpr int FEW_ROWS = 2048;
 
+/* Sequences up to which every wave finds its work by itself: past 192 k_paged_line pays (heads of 128, 32 on 8, up to 300 keys
+   of 2000: 192 sequences 43.4 us without it and 39.2, 1024 341 and 144, 4096 4264 and 569; 8 heads on 1 21.1 and 20.5, 85 and 31), in
+   a call that is otherwise one launch past 512 (up to 300 keys: 512 sequences 80.6 and 69.5, 8 heads on 1 16.4 and 17.8, 1024 187
+   and 133, 31.1 and 26.5). */
+constexpr int MANY = 192, MANY_WHOLE = 512;
+/* Bytes of the workspace that k_paged_line writes, before the parts; whole or not, as a call of fewer tokens may not be. */
+static size_t line_bytes(const wsr_paged& p) {
+    return p.n_seqs <= MANY ? 0 : (sizeof(Cut) + sizeof(Upto) * p.n_seqs + 255) / 256 * 256;
+}
+
 /* Rows of a tile: as many as a sequence's fill, on average; 128 where there are tiles enough of them (a chunk of 512 tokens of
    32 heads on 8, 128 tiles, 18.6 us with 128 rows and 15.5 with 64; two of up to 512 behind 4096, 216 tiles, 72 and 81), of
    heads of 256, whose workgroups are one to a CU, half as many (16 on 4: 4 chunks of up to 64, 32 tiles, 43 and 30; two of up to
@@ -509,10 +559,10 @@ static PagedPlan paged_plan(const wsr_paged& p) {
 /* What the call needs, and any of fewer tokens, whose tiles may be smaller and more. */
 size_t paged_workspace(const wsr_paged& p) {
     const PagedPlan pl = paged_plan(p);
-    if (p.max_len <= WHOLE) return 256;
+    if (p.max_len <= WHOLE) return std::max<size_t>(256, line_bytes(p));
     size_t rows = (size_t)pl.slots * pl.rows;
     for (int32_t r = 16; r < pl.rows; r *= 2) rows = std::max(rows, (size_t)(2 * held_of(r, p.head_dim) + SPARE) * r);
-    return rows * (p.head_dim + 4) * sizeof(float);
+    return line_bytes(p) + rows * (p.head_dim + 4) * sizeof(float);
 }
 
 /* Workgroups of the first launch. */
@@ -525,6 +575,11 @@ static hipError_t launch_dim(const wsr_paged& p, const PagedPlan& pl, hipStream_
     const dim3 grid((unsigned)blocks), threads(4 * WAVE);
     const bool once = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads) <= (int64_t)pl.rows * p.n_seqs;
     hipError_t e;
+    if (pl.line) {
+        hipLaunchKernelGGL(k_paged_line, dim3(1), dim3(NT), 0, s, p, pl);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     if (pl.rows > 32) {
         e = launch_paged_rows(p, pl, pl.rows / 32, once, blocks, s);
     } else {
@@ -549,7 +604,9 @@ static hipError_t launch_fmt(const wsr_paged& p, const PagedPlan& pl, hipStream_
 
 hipError_t launch_paged(const wsr_paged& p, void* ws, hipStream_t s) {
     PagedPlan pl = paged_plan(p);
-    pl.part = static_cast<float*>(ws);
+    char* at = static_cast<char*>(ws);
+    pl.part = reinterpret_cast<float*>(at + line_bytes(p));
+    if (p.n_seqs > (pl.whole ? MANY_WHOLE : MANY)) pl.line = reinterpret_cast<Line*>(at);
     return p.fmt == WSR_F16 ? launch_fmt<WSR_F16>(p, pl, s) : launch_fmt<WSR_BF16>(p, pl, s);
 }
 
