@@ -4,7 +4,8 @@ small random-weight decoder (head norms, rotary positions, grouped-query attenti
     python examples/paged_decode.py [--requests 24] [--tokens 40]
 
 A step feeds up to 16 tokens, what one weight pass takes: one of every request that is under way, and as much of the prompts of
-those that wait as fits.  Each request's keys lie in pages of one pool, taken when it needs them and given back when it is done.
+those that wait as fits.  Each request's keys lie in pages of one pool, taken when it needs them and given back when it is done;
+it begins when there is a place for it and the pool has pages for its whole answer beside those that others may still take.
 """
 from __future__ import annotations
 
@@ -150,17 +151,24 @@ class Server:
 
 
 def serve(server: Server, prompts: list[list[int]], n: int, each=None):
-    """Greedy answers of n tokens to every prompt, as many at a time as there are places.  Returns each prompt's tokens,
-    its own log probability (of all but its first token) and the answer's.  `each(requests, counts, tokens)` is called
-    after every step."""
+    """Greedy answers of n tokens to every prompt, in their order, as many at a time as there are places and pages for.
+    Returns each prompt's tokens, its own log probability (of all but its first token) and the answer's.
+    `each(requests, counts, tokens)` is called after every step."""
+    if n < 1 or not all(prompts) or server.seqs > MOST:
+        raise ValueError(f"prompts and answers have tokens, and a step has at most {MOST}, one of each place")
+    pages = [-(-(len(p) + n - 1) // server.page_size) for p in prompts]       # the last token's key is never stored
+    most, promised = len(server.free), 0
+    if max(pages, default=0) > min(most, server.row):
+        raise ValueError(f"a request of {max(pages)} pages, where the pool has {most} and a sequence {server.row}")
     stream, waiting = torch.cuda.current_stream(), list(range(len(prompts)))
     history, scored = [list(p) for p in prompts], [[0.0, 0.0] for _ in prompts]
     places: list[int | None] = [None] * server.seqs      # the request in each place, and what of it is cached
     cached = [0] * len(prompts)
     while waiting or any(r is not None for r in places):
         for b, r in enumerate(places):
-            if r is None and waiting:
+            if r is None and waiting and promised + pages[waiting[0]] <= most:
                 places[b] = waiting.pop(0)
+                promised += pages[places[b]]
         active = [r for r in places if r is not None]
         counts, room = [0] * server.seqs, MOST - len(active)
         for b, r in enumerate(places):                    # one token of each, and what fits of the prompts
@@ -189,7 +197,15 @@ def serve(server: Server, prompts: list[list[int]], n: int, each=None):
                 if len(history[r]) == len(prompts[r]) + n:
                     places[b] = None
                     server.hold(b, 0)
+                    promised -= pages[r]
     return history, scored
+
+
+def workload(requests: int, n: int):
+    """Prompts, and the sizes of a server that answers them with n tokens each: five places' worth of pages for its eight."""
+    prompts = [[(7 * i * i + r) % 61 for i in range(5 + 17 * r % 90)] for r in range(requests)]
+    longest = max(map(len, prompts)) + n
+    return prompts, dict(seqs=8, pages=5 * -(-longest // 16), page_size=16, longest=longest)
 
 
 def main():
@@ -197,9 +213,9 @@ def main():
     p.add_argument("--requests", type=int, default=24)
     p.add_argument("--tokens", type=int, default=40)
     o = p.parse_args()
-    server = Server(Model())
-    prompts = [[(7 * i * i + r) % 61 for i in range(5 + 17 * r % 90)] for r in range(o.requests)]
-    serve(server, prompts[:2], 2)
+    prompts, sizes = workload(o.requests, o.tokens)
+    server = Server(Model(), **sizes)
+    serve(server, prompts[:2], min(2, o.tokens))
     torch.cuda.synchronize()
     t0 = time.perf_counter()
     history, scored = serve(server, prompts, o.tokens)
