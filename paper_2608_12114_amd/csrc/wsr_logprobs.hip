@@ -170,8 +170,6 @@ __device__ __forceinline__ key64 largest_of(int count, int lane, const F& at) {
 __device__ __forceinline__ key64 lane_key(key64 v, int lane) {
     return (key64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
 }
-/* The wave's LDS stores are there for its loads that follow. */
-__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
 
 constexpr int ROOM = 5 * WAVE;                /* up to 63 that wait and four of each lane */
 

@@ -98,7 +98,9 @@ struct Walk {
             else to[i] = *at;
         }
     }
+    /* The block's rows are turned in LDS: keep_keys(), scores(), keep_values(), weigh(), each after a wave_fence(). */
     __device__ __forceinline__ void keep_keys(l_char* buf, int lane) const {
+        wave_fence();
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int key = AT_ONCE * i + lane / PIECES;
@@ -106,6 +108,7 @@ struct Walk {
         }
     }
     __device__ __forceinline__ void keep_values(l_char* buf, int lane) const {
+        wave_fence();
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int key = AT_ONCE * i + lane / PIECES;
@@ -114,6 +117,7 @@ struct Walk {
     }
 
     __device__ __forceinline__ void scores(f4_t (&s)[RT][2], const l_char* buf, int lane) const {
+        wave_fence();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -132,6 +136,7 @@ struct Walk {
                                           const l_char* buf, int lane) {
         const int g = lane / 16;
         u32x4 pt[RT];
+        wave_fence();
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             if (masked) {
@@ -325,6 +330,7 @@ __global__ __launch_bounds__(NW * WAVE) __attribute__((amdgpu_waves_per_eu(waves
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         if (t) __syncthreads();
+        else wave_fence();
         l_char* mine = lds + wave * W::ROOM;
 #pragma unroll
         for (int i = 0; i < W::DT; ++i) *(l_f4*)(mine + (i * WAVE + lane) * 16) = w.o[t][i];

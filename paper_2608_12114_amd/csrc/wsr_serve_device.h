@@ -22,6 +22,11 @@ using wsr_step::unpack8;
 constexpr float NEG_INF = -__builtin_inff();
 constexpr float LOG2E = 1.4426950408889634f;
 
+/* Lanes of a wave hand each other values through LDS: what was stored is there for the loads that follow, what was loaded has
+   been read before the stores that follow.  No instruction, as a wave's LDS operations are done in order; the compiler may not
+   move them across. */
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
+
 /* The sequence that row `tok` belongs to (-1: none) and the row behind its last: the last sequence that starts at or before
    it, by a search of 64 samples at a time (one load's latency below 64 sequences, two below 4096).  By whole waves, tok
    uniform. */
