@@ -234,6 +234,10 @@ __device__ __forceinline__ void finish(const wsr_logprobs& p, int64_t r, float t
     if (p.entropy) p.entropy[r] = t == 0.f || st.m == NEG_INF ? 0.f : fmaxf(log_s - 0.6931471805599453f * (st.e / st.s), 0.f);
 }
 
+/* What the waves of a workgroup show each other without a barrier. */
+__device__ __forceinline__ float seen(const float* at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ void show(float* at, float v) { __hip_atomic_store(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+
 /* TOP: no alternatives, one, or up to 8, 32 or 64.  VU: 16-byte loads per thread of a chunk. */
 template <int VU, int TOP>
 __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_logprobs(wsr_logprobs p, LogPlan pl) {
@@ -342,13 +346,15 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_
                 const int order = __builtin_bit_cast(int, sorted<WAVE>(m, true, lane));
                 const float bar = __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, p.n_top - 1));
                 if (bar > NEG_INF) b.raise(key_of(bar, -1));
-                if (lane == 0) quarter[wave] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, fourth));
+                if (lane == 0) show(&quarter[wave], __builtin_bit_cast(float, __builtin_amdgcn_readlane(order, fourth)));
                 if (c == begin) __syncthreads();
             }
-            /* four waves that have seen n / 4 logits of at least this: no smaller one is among the workgroup's n */
-            float common = quarter[0];
+            /* four waves that have seen n / 4 logits of at least this: no smaller one is among the workgroup's n.  The waves
+               write theirs at any time: whichever of a wave's values is read, it has seen n / 4 logits of at least that, so that
+               the results do not depend on it. */
+            float common = seen(&quarter[0]);
 #pragma unroll
-            for (int w = 1; w < LW; ++w) common = fminf(common, quarter[w]);
+            for (int w = 1; w < LW; ++w) common = fminf(common, seen(&quarter[w]));
             if (common > b.bar) b.raise(key_of(common, -1));
             if (__ballot(top >= b.bar && top > NEG_INF))
 #pragma unroll
@@ -356,7 +362,7 @@ __global__ __launch_bounds__(LT) __attribute__((amdgpu_waves_per_eu(6))) void k_
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         if (__ballot(v[u][j] >= b.bar)) b.add(key_of(v[u][j], i0 + u * LT * 4 + j), v[u][j] > NEG_INF, lane);
-                    if (b.drain(lane) && lane == fourth) quarter[wave] = logit_of(b.best);
+                    if (b.drain(lane) && lane == fourth) show(&quarter[wave], logit_of(b.best));
                 }
         }
     }
