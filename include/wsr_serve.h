@@ -103,7 +103,7 @@ wsr_status wsr_append_qkv(const wsr_qkv* p, void* stream);
    times heads at most 2^25; n_kv_heads * (n_seqs + a key head's rows / 16) past 2^23 may be refused.  head_dim 64, 128
    or 256; every pointer 16-byte aligned and every stride a multiple of 16 (of 4 for table, starts, lens and lse); lse
    (n_tokens, n_heads) or null; out and lse overlap nothing.  Sums of probabilities, relative to within 2^8 of the largest,
-   times values are infinite past fp32's range.
+   times values are infinite past fp32's range.  scale is above 0 and at most 2^127.
    ws: wsr_paged_workspace_bytes(), 256-byte aligned; what it gives serves calls of fewer tokens too where the rest is the
    same (without starts, of fewer sequences). */
 typedef struct wsr_paged {

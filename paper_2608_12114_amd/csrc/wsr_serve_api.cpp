@@ -146,7 +146,9 @@ static wsr_status check_paged(const wsr_paged& p, const char* who) {
     if (p.n_seqs < 0 || p.n_tokens < 0 || p.max_len < 0 || p.reserved) return fail(WSR_E_ARG, "%s: negative size", who);
     if (p.n_tokens > 1 << 20 || p.n_seqs > 1 << 20) return fail(WSR_E_SIZE, "%s: too many tokens or sequences", who);
     if ((int64_t)p.n_tokens * p.n_heads > 1 << 25) return fail(WSR_E_SIZE, "%s: tokens times heads above 2^25", who);
-    if (!(p.scale > 0.f) || !std::isfinite(p.scale)) return fail(WSR_E_ARG, "%s: scale must be positive and finite", who);
+    /* the kernels take powers of two: scale log2 e is finite too */
+    if (!(p.scale > 0.f) || !std::isfinite(p.scale * 1.4426950408889634f))
+        return fail(WSR_E_ARG, "%s: scale must be positive, and finite times log2 e", who);
     if (!p.starts && p.n_tokens != p.n_seqs) return fail(WSR_E_ARG, "%s: without starts each sequence has one token", who);
     if (p.n_seqs == 0 && p.n_tokens > 0) return fail(WSR_E_ARG, "%s: tokens of no sequence", who);
     WSR_TRY(check_pages(p.cache, p.n_seqs, p.n_kv_heads, who));
