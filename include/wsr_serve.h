@@ -60,7 +60,8 @@ typedef struct wsr_pages {
    positions: device int32 (n_axes, n_tokens), or null: the token's place (n_axes 1).  axis_of: device int32
    [rot_dim / 2], clamped to [0, n_axes), or null (all 0).  freqs: device fp32 [rot_dim / 2].
    Tokens of no sequence, and places below 0, past the table's row or in holes, are not stored, and nothing else is
-   changed; a token's query does not depend on its place being there.  Two tokens in the same slot leave either.
+   changed; a token's query does not depend on its place being there.  Two tokens in the same slot, the one case whose result is
+   not the same every time, leave some values of each there.  A norm's squares past fp32's range are infinite, its head 0.
    q may be null (nothing but the cache), or k and v (nothing but queries; the cache may be all 0).
    head_dim 64, 128 or 256; rot_dim % 8 == 0, at most head_dim; n_axes 1 to 4; n_tokens and n_seqs at most 2^20, n_heads
    at most 4096 (n_kv_heads too; neither need divide the other here); inputs, weights and q_out 16-byte aligned,
@@ -94,8 +95,8 @@ wsr_status wsr_append_qkv(const wsr_qkv* p, void* stream);
    Sequence b's query tokens are rows starts[b] .. starts[b + 1] - 1 of q (starts null: one each, row b), the last n_b of
    its lens[b] places: query i sees keys j < lens[b] - n_b + i + 1 on pages that are no holes,
      out = sum_k softmax_k(scale q . key_k) value_k,  lse = log sum_k exp(scale q . key_k).
-   A row that sees no key gets out = 0 and lse = -inf, one with a NaN among its scores NaN in both; keys past lens[b] and in
-   holes are never read into a result.  Query head h reads key head h / (n_heads / n_kv_heads).  Types `fmt`; scores, softmax
+   A row that sees no key, or none with a score above -inf, gets out = 0 and lse = -inf, one with a NaN (or +inf) among its
+   scores NaN in both; keys past lens[b] and in holes are never read into a result.  Query head h reads key head h / (n_heads / n_kv_heads).  Types `fmt`; scores, softmax
    statistics and sums are fp32, probabilities are rounded to `fmt` for the product with the values, out once to `fmt`.
    Rows of q that belong to no sequence (before starts[0], from starts[n_seqs] on) keep what out and lse held.
    starts: device int32 [n_seqs + 1], not decreasing, clamped to [0, n_tokens]; lens: device int32 [n_seqs], clamped to
