@@ -105,6 +105,8 @@ wsr_status wsr_append_qkv(const wsr_qkv* p, void* stream);
    or 256; every pointer 16-byte aligned and every stride a multiple of 16 (of 4 for table, starts, lens and lse); lse
    (n_tokens, n_heads) or null; out and lse overlap nothing.  Sums of probabilities, relative to within 2^8 of the largest,
    times values are infinite past fp32's range.  scale is above 0 and at most 2^127.
+   Tiles of rows are as high as the call's mean sequence fills: many sequences without tokens beside a few long chunks cost
+   time, and are better left out.
    ws: wsr_paged_workspace_bytes(), 256-byte aligned; what it gives serves calls of fewer tokens too where the rest is the
    same (without starts, of fewer sequences). */
 typedef struct wsr_paged {

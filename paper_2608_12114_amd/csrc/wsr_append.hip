@@ -12,7 +12,7 @@
  * more, so that far positions lose nothing before that part becomes fp32.
  *
  * Bound by HBM for prompts: 6300 tokens of 48 heads of 128, 241 MB, 49 us, 4.9 TB/s (a copy of 1 GiB 4.8), by a launch and one
- * chain of loads for few tokens: one token 4.1 us in a graph, 64 of 80 heads 5.2.
+ * chain of loads for few tokens: one token 4.2 us in a graph, 64 of 80 heads 5.3.
  */
 #include <hip/hip_runtime.h>
 

@@ -61,8 +61,10 @@ __device__ __forceinline__ Seq seq_at(const wsr_paged& p, int R, int b) {
    graph, in one and a half rounds 267; 24 of 5 drafts of 8 heads 63, by the other rule 74).  Otherwise parts are half of what
    falls to a workgroup, and units of less than two such stay whole, so that whoever is done early takes another (16 sequences
    of 2000 with 32 key heads 58 us, by the first rule 67; 32 of up to 4096 63, with parts two thirds or four thirds as long 65).
-   A part has 256 keys or more, of 64 (128) rows 448 (704), since its rows have to be written and read again.  Sums of lengths
-   are fp32, with every product's rounding written out: all waves of both kernels have to cut alike. */
+   Parts are meant to have 256 keys or more, of 64 (128) rows 448 (704), since their rows have to be written and read again; as
+   their number is rounded up where units are few, and a unit's keys are shared out in whole rounds of its workgroup's blocks,
+   the last ones may have a few keys or none (of 257 keys 256 and 1; 32771 are 95 parts, of which 85 have 384, one the rest).
+   Sums of lengths are fp32, with every product's rounding written out: all waves of both kernels have to cut alike. */
 struct Sums {
     float keys, units;
     __device__ __forceinline__ void add(const Seq& s, int N) {

@@ -11,7 +11,10 @@
  *
  *   S^T = K Q^T   (v_mfma 16x16x32: 16 keys x 16 rows, each lane one row and four keys)
  *   P   = exp2((S - max) scale log2 e),  O^T += V^T P^T with P still in the registers of S: the lane layout of S^T is
- *         the operand layout of P^T when V's keys are taken in the same order
+ *         the operand layout of P^T when V's keys are taken in the same order.  P is rounded to the values' 16 bits, as the
+ *         instruction takes both operands in one type, and its sum is not: in f16 0.00025 to 0.00027 from 64 bits where
+ *         outputs alone are 0.00021, in bf16 0.0019 to 0.0022 and 0.0017.  (A second operand with P's rest would leave the
+ *         latter for twice these products.)
  *
  * Keys and values are loaded as whole rows, a wave's 64 lanes of 16 bytes side by side, into registers, which hold more on
  * their way than LDS could, and turned into operands by the wave's own 32 rows of LDS: first the keys, then, by transposing
@@ -45,7 +48,7 @@ constexpr float LAZY = 8.f;
 
 /* ---- a wave's walk ----------------------------------------------------------------------------------- */
 
-template <int FMT, int D, int RT, bool ONCE>  /* RT: tiles of 16 rows; ONCE: nobody else reads the keys */
+template <int FMT, int D, int RT, bool ONCE>  /* RT: tiles of 16 rows; ONCE: hinted that keys are read once */
 struct Walk {
     static constexpr int KS = D / 32, DT = D / 16, R = 16 * RT;
     static constexpr int PIECES = D / 8, ROW = 2 * D;           /* 16-byte pieces of a key, and its bytes */
@@ -528,7 +531,8 @@ static size_t line_bytes(const wsr_paged& p) {
     return p.n_seqs <= MANY ? 0 : (sizeof(Cut) + sizeof(Upto) * p.n_seqs + 255) / 256 * 256;
 }
 
-/* Rows of a tile: as many as a sequence's fill, on average; 128 where there are tiles enough of them (a chunk of 512 tokens of
+/* Rows of a tile, one height for the whole call, as the host does not know which sequence has how many: as many as a sequence's
+   fill, on average; 128 where there are tiles enough of them (a chunk of 512 tokens of
    32 heads on 8, 128 tiles, 18.6 us with 128 rows and 15.5 with 64; two of up to 512 behind 4096, 216 tiles, 72 and 81), of
    heads of 256, whose workgroups are one to a CU, half as many (16 on 4: 4 chunks of up to 64, 32 tiles, 43 and 30; two of up to
    512 behind 4096, 108 tiles, 87 and 112, with 32 rows 173). */
@@ -579,6 +583,8 @@ template <int FMT, int D>
 static hipError_t launch_dim(const wsr_paged& p, const PagedPlan& pl, hipStream_t s) {
     const int64_t blocks = paged_blocks(p, pl);
     const dim3 grid((unsigned)blocks), threads(4 * WAVE);
+    /* whether a sequence's rows are one tile, on average: the hint that its keys are read once, right for most of them then.  Of
+       others it costs time alone (63 tokens and a chunk of 200 of 32 heads on 8 154 us, in two calls 149). */
     const bool once = (int64_t)p.n_tokens * (p.n_heads / p.n_kv_heads) <= (int64_t)pl.rows * p.n_seqs;
     hipError_t e;
     if (pl.line) {

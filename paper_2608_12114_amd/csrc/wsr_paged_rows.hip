@@ -24,7 +24,7 @@ using wsr_step::l_char;
 
 typedef __attribute__((address_space(1))) const char g_char;
 
-template <int FMT, int D, int RW, bool ONCE>  /* ONCE: nobody else reads the keys */
+template <int FMT, int D, int RW, bool ONCE>  /* ONCE: hinted that keys are read once */
 struct PagedBlocks : wsr_step::AttendBlocks<FMT, D, RW> {
     typedef wsr_step::AttendBlocks<FMT, D, RW> B;
     using B::HALF, B::KS, B::DT, B::KT, B::KW, B::LOADS, B::PIECES, B::BUFFER, B::q, B::o, B::m, B::kswz, B::vswz, B::step;
