@@ -96,8 +96,9 @@ wsr_status wsr_append_qkv(const wsr_qkv* p, void* stream);
    its lens[b] places: query i sees keys j < lens[b] - n_b + i + 1 on pages that are no holes,
      out = sum_k softmax_k(scale q . key_k) value_k,  lse = log sum_k exp(scale q . key_k).
    A row that sees no key, or none with a score above -inf, gets out = 0 and lse = -inf, one with a NaN (or +inf) among its
-   scores NaN in both; keys past lens[b] and in holes are never read into a result.  Query head h reads key head h / (n_heads / n_kv_heads).  Types `fmt`; scores, softmax
-   statistics and sums are fp32, probabilities are rounded to `fmt` for the product with the values, out once to `fmt`.
+   scores NaN in both; keys past lens[b] and in holes are never read into a result.  Query head h reads key head
+   h / (n_heads / n_kv_heads).  Types `fmt`; scores, softmax statistics and sums are fp32, probabilities are rounded to `fmt`
+   for the product with the values, out once to `fmt`.
    Rows of q that belong to no sequence (before starts[0], from starts[n_seqs] on) keep what out and lse held.
    starts: device int32 [n_seqs + 1], not decreasing, clamped to [0, n_tokens]; lens: device int32 [n_seqs], clamped to
    [0, max_len]; max_len <= max_pages * page_size.  n_tokens and n_seqs at most 2^20, n_heads at most 4096, tokens
