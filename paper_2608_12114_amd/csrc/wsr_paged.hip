@@ -388,7 +388,7 @@ __global__ __launch_bounds__(NW * WAVE) __attribute__((amdgpu_waves_per_eu(waves
 constexpr int NT = 1024, NW = NT / WAVE;
 __global__ __launch_bounds__(NT) void k_paged_line(wsr_paged p, PagedPlan pl) {
     __shared__ float keys[NW], units[NW];
-    __shared__ int64_t all[2][NW], cuts[2][NW];                 /* of the waves, of this round and the one before */
+    __shared__ int64_t all[2][NW], cuts[2][NW];                 /* of the waves, of one pass of the loop and the next */
     const int lane = threadIdx.x % WAVE, wave = wsr::wave_in_block(), N = p.n_kv_heads;
     Cut cut{1.f, 0.f};
     if (!pl.whole) {
